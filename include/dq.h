@@ -65,6 +65,7 @@ typedef enum { DQ_KIND_DQSG = 0, DQ_KIND_NDQSG = 1 } dq_kind;
                                           was skipped and its outputs are undefined                        */
 #define DQ_WARN_CODE_RANGE      0x4u   /* dq_ternary_pack met a code 3 (not a three-level message); it was
                                           stored as 2                                                      */
+#define DQ_WARN_NONFINITE_NORM  0x8u   /* a gradient norm was NaN or Inf                                   */
 
 /* One quantizer description.  Plain data, read during the call. */
 typedef struct {
@@ -275,6 +276,97 @@ uint64_t dq_ternary_bytes(uint64_t n);
 dq_status dq_ternary_pack(const uint32_t* packed, uint64_t n, uint8_t* out_radix, uint32_t* status_word,
                           void* cuda_stream);
 dq_status dq_ternary_unpack(const uint8_t* radix, uint64_t n, uint32_t* out_packed, void* cuda_stream);
+
+/*
+ * Gradients of many tensors.  A training program holds its gradient as a list of tensors, often in 16-bit types; the
+ * encoders take, and the decoders give, one flat fp32 vector.  The calls below do what happens to the list around the
+ * exchange: its global norm, clipping by it, and the way into the flat vector and back, clipped on the way.
+ * (The paper has no counterpart; its kappa = ||g||_inf of a whole gradient is the norm of kind DQ_NORM_MAX.)
+ *
+ * A tensor is n elements of one type in rows of `row` contiguous elements, `row_stride` elements from the start of one
+ * row to that of the next (a column block of a larger matrix); row = 0 says that all of it is contiguous.  `data` needs
+ * the alignment of its type only.  Tensors may be empty, and a list may be.
+ */
+typedef enum { DQ_F32 = 0, DQ_BF16 = 1, DQ_F16 = 2 } dq_dtype;
+
+typedef struct {
+    void*    data;        /* device; not written where the tensor is an input; may be NULL when n = 0          */
+    uint64_t n;           /* elements                                                                         */
+    uint64_t row;         /* elements per row, a divisor of n below 2^31; 0: contiguous                        */
+    uint64_t row_stride;  /* row <= row_stride < 2^32; ignored when row = 0                                    */
+    dq_dtype dtype;
+    uint32_t reserved;    /* 0                                                                                */
+} dq_tensor;
+
+typedef enum {
+    DQ_NORM_L2 = 0,       /* sqrt(sum of squares), summed in fp64 and rounded once to fp32                      */
+    DQ_NORM_MAX = 1       /* max |x|                                                                          */
+} dq_norm;
+
+/*
+ * How a list is clipped: every element is multiplied in fp32 by c = 1 if N <= max_norm, else max_norm / N, and rounded once
+ * to the destination's type.  N is the norm that the call computes of its input, or the one at `norm` (for instance of
+ * all ranks' parts together).  A norm of Inf gives c = 0, a NaN gives c = NaN; finite gradients whose L2 norm is beyond
+ * the fp32 range have the norm Inf.
+ */
+typedef struct {
+    float        max_norm;     /* >= 0; Inf: nothing is clipped                                                */
+    dq_norm      kind;         /* of the norm that the call computes                                          */
+    const float* norm;         /* device, fp32[1]: the norm to clip by; NULL: the call computes it             */
+    float*       out_norm;     /* device, fp32[1], optional: receives N, the norm before clipping            */
+    uint32_t*    status_word;  /* device, optional: DQ_WARN_NONFINITE_NORM is OR-ed into it                    */
+} dq_clip;
+
+#define DQ_MAX_TENSORS 65536u
+
+/*
+ * Device memory that the calls below want as `workspace` for this list (the input list; dq_grad_scatter: the outputs),
+ * 16-byte aligned; 0 for short lists, where it may be NULL.  It holds nothing between calls; calls that may overlap in
+ * time need one each.  each != 0: for dq_grad_norm with out_norms.  0 also for a list that the calls refuse.
+ */
+uint64_t dq_grad_workspace_bytes(const dq_tensor* list, uint32_t count, int each);
+
+/*
+ * dq_grad_norm -- the norm over all elements of all tensors.
+ *   grads        host array of `count` tensors (<= DQ_MAX_TENSORS, fewer than 2^34 elements together), read during the
+ *                call; the tensors may overlap
+ *   out_norm     device, fp32[1]; 0 for an empty list
+ *   out_norms    device, fp32[count], optional: the norm of each tensor (0 for an empty one)
+ *   status_word  device uint32, optional: DQ_WARN_NONFINITE_NORM is OR-ed into it when the norm is NaN or Inf
+ */
+dq_status dq_grad_norm(const dq_tensor* grads, uint32_t count, dq_norm kind, float* out_norm, float* out_norms,
+                       uint32_t* status_word, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * dq_grad_clip -- clips a list.
+ *   out   host array of `count` tensors of the same sizes as the inputs', of any of the types, or NULL: in place, where
+ *         a list within the limit is neither read again nor written.  Element i of a tensor in row order goes to element
+ *         i; where input and output both have rows (row_stride > row), these are equally long, else DQ_ERR_UNSUPPORTED.
+ *         Outputs (out_norm and status_word are among them) overlap neither each other nor the inputs, and in place no two
+ *         tensors overlap (the same one twice would be scaled twice): DQ_ERR_INVALID_ARG.  (Blocks of rows of different strides whose spans interleave count as
+ *         overlapping.)
+ * A bucket scale of a message is linear in the gradient, so clipping a message's out_scale by the gradient's norm
+ * (`norm`) gives the message of the clipped gradient without touching the gradient or the codes.
+ */
+dq_status dq_grad_clip(const dq_tensor* grads, uint32_t count, const dq_clip* clip, const dq_tensor* out, void* workspace,
+                       uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * dq_grad_gather -- a list into the flat fp32 vector that an encoder takes: the tensors in list order, each in row order.
+ *   clip      NULL: nothing is clipped and no norm computed
+ *   out_flat  device, fp32[sum of n], 16-byte aligned, fully overwritten; overlaps no input
+ */
+dq_status dq_grad_gather(const dq_tensor* grads, uint32_t count, const dq_clip* clip, float* out_flat, void* workspace,
+                         uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * dq_grad_scatter -- a flat fp32 vector, such as a decoded mean, into a list: the reverse of dq_grad_gather.
+ *   flat  device, fp32[sum of n], 16-byte aligned; overlaps no output
+ *   clip  as above; the norm is that of flat
+ *   out   host array of `count` tensors, of any of the types, fully overwritten; they do not overlap
+ */
+dq_status dq_grad_scatter(const float* flat, const dq_clip* clip, const dq_tensor* out, uint32_t count, void* workspace,
+                          uint64_t workspace_bytes, void* cuda_stream);
 
 /*
  * Host-buffer variants.  Every data pointer (grad, out_packed, out_scale, the packed/scale pointers

@@ -21,6 +21,10 @@ DQ_KIND_NDQSG = 1
 DQ_WARN_NONFINITE_SCALE = 0x1
 DQ_ERR_COPY_TIMEOUT = 0x2
 DQ_WARN_CODE_RANGE = 0x4
+DQ_WARN_NONFINITE_NORM = 0x8
+DQ_NORM_L2 = 0
+DQ_NORM_MAX = 1
+DQ_F32, DQ_BF16, DQ_F16 = 0, 1, 2
 DQ_FLAG_INPUT_READY = 0x1
 DQ_FLAG_OUTPUT_FREE = 0x2
 DQ_FLAG_TEST_DROP_COPY = 0x80000000
@@ -44,6 +48,16 @@ class DqParams(C.Structure):
 class DqMsg(C.Structure):
     _fields_ = [("packed", C.c_void_p), ("scale", C.c_void_p), ("seed", C.c_uint64),
                 ("worker", C.c_uint32), ("kind", C.c_int), ("p", DqParams)]
+
+
+class DqTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n", C.c_uint64), ("row", C.c_uint64), ("row_stride", C.c_uint64),
+                ("dtype", C.c_int), ("reserved", C.c_uint32)]
+
+
+class DqClip(C.Structure):
+    _fields_ = [("max_norm", C.c_float), ("kind", C.c_int), ("norm", C.c_void_p), ("out_norm", C.c_void_p),
+                ("status_word", C.c_void_p)]
 
 
 _lib = None
@@ -87,6 +101,12 @@ def lib() -> C.CDLL:
         L.dq_ternary_bytes.argtypes = [u64]; L.dq_ternary_bytes.restype = u64
         L.dq_ternary_pack.argtypes = [vp, u64, vp, vp, vp]; L.dq_ternary_pack.restype = C.c_int
         L.dq_ternary_unpack.argtypes = [vp, u64, vp, vp]; L.dq_ternary_unpack.restype = C.c_int
+        pt, pc = C.POINTER(DqTensor), C.POINTER(DqClip)
+        L.dq_grad_workspace_bytes.argtypes = [pt, u32, C.c_int]; L.dq_grad_workspace_bytes.restype = u64
+        L.dq_grad_norm.argtypes = [pt, u32, C.c_int, vp, vp, vp, vp, u64, vp]; L.dq_grad_norm.restype = C.c_int
+        L.dq_grad_clip.argtypes = [pt, u32, pc, pt, vp, u64, vp]; L.dq_grad_clip.restype = C.c_int
+        L.dq_grad_gather.argtypes = [pt, u32, pc, vp, vp, u64, vp]; L.dq_grad_gather.restype = C.c_int
+        L.dq_grad_scatter.argtypes = [vp, pc, pt, u32, vp, u64, vp]; L.dq_grad_scatter.restype = C.c_int
         L.dq_encode_workspace_bytes.argtypes = [u64, pp]; L.dq_encode_workspace_bytes.restype = u64
         L.dq_decode_workspace_bytes.argtypes = [pm, u32, u64, C.c_int]; L.dq_decode_workspace_bytes.restype = u64
         for f in (L.dqsg_encode_host, L.ndqsg_encode_host):
@@ -386,6 +406,70 @@ def ternary_unpack(data: torch.Tensor, n: int, out: Optional[torch.Tensor] = Non
         with _allocating_for(stream, data.device):
             out = new_output(max(1, packed_words(n, 2)), torch.int32, data.device)
     _check((_calls_module or _calls()).ternary_unpack(data, n, out, stream), "dq_ternary_unpack")
+    return out
+
+
+# ------------------------------------------------------------------------------------------ gradients of many tensors
+# The tensors of a list are fp32, bf16 or fp16, of any mix, sizes and alignment, all on one device, which need not be the
+# current one (without `stream` a call runs on that device's current stream).  They may be column blocks: rows of
+# contiguous elements at one distance; where the order of the elements does not matter (grad_norm, grad_clip in place or
+# into tensors of the same strides) any dense tensor will do.  Norms are fp32 tensors of one element on the device;
+# nothing is synchronised.
+def _one_on(stream, tensors, what):
+    if not len(tensors):
+        raise ValueError(f"{what}: an empty list needs its output tensor")
+    with _allocating_for(stream, tensors[0].device):
+        return new_output(1, torch.float32, tensors[0].device)
+
+
+def grad_norm(grads: Sequence[torch.Tensor], kind: int = DQ_NORM_L2, out_norm: Optional[torch.Tensor] = None,
+              out_norms: Optional[torch.Tensor] = None, status_word: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """The norm over all elements of all tensors (DQ_NORM_L2 or DQ_NORM_MAX).  `out_norms` (fp32, one element per tensor)
+    receives the norm of each tensor as well; DQ_WARN_NONFINITE_NORM is OR-ed into `status_word` when the norm is NaN or
+    Inf."""
+    if out_norm is None:
+        out_norm = _one_on(stream, grads, "grad_norm")
+    _check((_calls_module or _calls()).grad_norm(grads, kind, out_norm, out_norms, status_word, stream), "dq_grad_norm")
+    return out_norm
+
+
+def grad_clip(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+              norm: Optional[torch.Tensor] = None, kind: int = DQ_NORM_L2, out_norm: Optional[torch.Tensor] = None,
+              status_word: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Multiplies every element by min(1, max_norm / N), in place or into the tensors of `out` (same shapes, any types).
+    N, which is returned, is the norm of `grads`, or `norm` where that is given.  ``grad_clip([scale], max_norm,
+    norm=N)`` clips a message instead of its gradient."""
+    if out_norm is None and norm is None:
+        out_norm = _one_on(stream, grads, "grad_clip")
+    _check((_calls_module or _calls()).grad_clip(grads, max_norm, out, norm, kind, out_norm, status_word, stream),
+           "dq_grad_clip")
+    return norm if out_norm is None else out_norm
+
+
+def grad_gather(grads: Sequence[torch.Tensor], out_flat: Optional[torch.Tensor] = None, max_norm: Optional[float] = None,
+                norm: Optional[torch.Tensor] = None, kind: int = DQ_NORM_L2, out_norm: Optional[torch.Tensor] = None,
+                status_word: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The tensors, one after the other, as the flat fp32 vector that an encoder takes; clipped on the way if `max_norm` is
+    given (`norm`, `kind`, `out_norm` and `status_word` as in grad_clip)."""
+    if out_flat is None:
+        if not len(grads):
+            raise ValueError("grad_gather: an empty list needs its output tensor")
+        n = sum(g.numel() for g in grads)
+        with _allocating_for(stream, grads[0].device):
+            out_flat = new_output(max(1, n), torch.float32, grads[0].device)
+    _check((_calls_module or _calls()).grad_gather(grads, out_flat, max_norm, norm, kind, out_norm, status_word, stream),
+           "dq_grad_gather")
+    return out_flat
+
+
+def grad_scatter(flat: torch.Tensor, out: Sequence[torch.Tensor], max_norm: Optional[float] = None,
+                 norm: Optional[torch.Tensor] = None, kind: int = DQ_NORM_L2, out_norm: Optional[torch.Tensor] = None,
+                 status_word: Optional[torch.Tensor] = None, stream=None) -> Sequence[torch.Tensor]:
+    """A flat fp32 vector, such as a decoded mean, into the tensors of `out`; clipped on the way if `max_norm` is given, by
+    the norm of `flat` or by `norm`."""
+    _check((_calls_module or _calls()).grad_scatter(flat, out, max_norm, norm, kind, out_norm, status_word, stream),
+           "dq_grad_scatter")
     return out
 
 

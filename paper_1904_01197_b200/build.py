@@ -31,7 +31,7 @@ NVCC_FLAGS = [
 ]
 
 # (object name, source, extra defines)
-UNITS = [("dq_b200", "dq_b200.cu", [])]
+UNITS = [("dq_b200", "dq_b200.cu", []), ("dq_grad", "dq_grad.cu", [])]
 UNITS += [(f"enc_m{m}_d{d}", "dq_encode_inst.cu", [f"-DDQ_INST_MODE={m}", f"-DDQ_INST_DITH={d}"])
           for m in (0, 1, 2, 3) for d in (32, 16)]
 UNITS += [(f"dec_d{d}_r{r}_e{e}", "dq_decode_inst.cu", [f"-DDQ_INST_DITH={d}", f"-DDQ_INST_RUN={r}", f"-DDQ_INST_E={e}"])

@@ -22,10 +22,33 @@
 static __device__ unsigned int g_dq_error_flags = 0u;
 
 namespace {
-
-using dq::launch_overlapped;
-
 std::atomic<uint64_t> g_launches{0};
+}  // namespace
+
+namespace dq {
+
+void count_launch() { g_launches.fetch_add(1); }
+
+int device_sm_count()
+{
+    static thread_local int cached_dev = -1, cached_sms = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev != cached_dev) {
+        int sms = 0;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        cached_dev = dev;
+        cached_sms = sms;
+    }
+    return cached_sms;
+}
+
+}  // namespace dq
+
+namespace {
+
+using dq::device_sm_count;
+using dq::launch_overlapped;
 
 bool is_pow2(uint32_t v) { return v && !(v & (v - 1u)); }
 
@@ -62,20 +85,6 @@ void fill_philox(dq::PhiloxStream& ps, uint64_t seed, uint32_t worker, uint64_t 
     ps.v3 = (uint32_t)p0 ^ k[2][1];
     ps.k2 = k[2][0];
     std::memcpy(ps.rk, k + 3, sizeof(ps.rk));
-}
-
-int device_sm_count()
-{
-    static thread_local int cached_dev = -1, cached_sms = 0;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    if (dev != cached_dev) {
-        int sms = 0;
-        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-        cached_dev = dev;
-        cached_sms = sms;
-    }
-    return cached_sms;
 }
 
 dq_status check_params(const dq_params* p, dq_kind kind, uint32_t* levels_out, float* alpha_out)

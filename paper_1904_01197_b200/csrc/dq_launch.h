@@ -12,6 +12,10 @@
 
 namespace dq {
 
+// Shared by the translation units of the C ABI's host side (defined in dq_b200.cu).
+int device_sm_count();          // of the current device; 0 on a CUDA error
+void count_launch();            // one more in dq_launch_count
+
 struct EncodeArgs;
 struct DirectArgs;
 template <int MAXW> struct DecodeArgsOf;

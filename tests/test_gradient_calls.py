@@ -1,0 +1,231 @@
+"""Calls on gradients of many tensors, without a GPU: what the C ABI refuses before it launches anything, what the binding
+refuses, and the sizes of the workspace."""
+import ctypes as C
+import subprocess
+import sys
+from pathlib import Path
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+OK, INVALID, UNSUPPORTED, ALIGNMENT = 0, 1, 2, 3
+BASE = 0x100000                     # never dereferenced: checks come first
+MANY = 1 << 20                      # elements: more than one launch takes, so that a workspace is needed
+
+
+@pytest.fixture(scope="module")
+def dq():
+    from paper_1904_01197_b200 import build
+    build.build()
+    import paper_1904_01197_b200 as dq
+    return dq
+
+
+def _list(dq, *tensors):
+    return (dq.DqTensor * max(1, len(tensors)))(*tensors)
+
+
+def _t(dq, data=BASE, n=MANY, row=0, stride=0, dtype=0, reserved=0):
+    return dq.DqTensor(data, n, row, stride, dtype, reserved)
+
+
+def _clip(dq, max_norm=1.0, kind=0, norm=None, out_norm=0x40, status=None):
+    return C.byref(dq.DqClip(max_norm, kind, norm, out_norm, status))
+
+
+WS = dict(ws=0x200, bytes=1 << 30)
+
+
+def test_struct_layout_matches_header(dq):
+    assert C.sizeof(dq.DqTensor) == 40 and dq.DqTensor.dtype.offset == 32
+    assert C.sizeof(dq.DqClip) == 32 and dq.DqClip.norm.offset == 8
+
+
+BAD_TENSORS = [
+    (dict(dtype=3), INVALID),
+    (dict(dtype=-1), INVALID),
+    (dict(reserved=1), INVALID),
+    (dict(data=None), INVALID),
+    (dict(n=1 << 34), UNSUPPORTED),
+    (dict(data=BASE + 2), ALIGNMENT),                       # fp32 at an address of two bytes
+    (dict(data=BASE + 1, dtype=1), ALIGNMENT),
+    (dict(row=3), INVALID),                                 # no whole number of rows
+    (dict(row=1024, stride=1023), INVALID),                 # rows that overlap
+    (dict(row=1024, stride=0), INVALID),
+    (dict(n=1 << 33, row=1 << 31, stride=(1 << 31) + 1), UNSUPPORTED),
+    (dict(row=1024, stride=1 << 32), UNSUPPORTED),
+]
+
+
+@pytest.mark.parametrize("kw,want", BAD_TENSORS, ids=[str(k) for k, _ in BAD_TENSORS])
+def test_a_bad_tensor_is_refused_by_every_call(dq, kw, want):
+    L = dq.lib()
+    before = L.dq_launch_count()
+    bad, good = _list(dq, _t(dq, data=BASE << 8), _t(dq, **kw)), _list(dq, _t(dq, data=BASE << 8), _t(dq, data=BASE << 12))
+    flat = BASE << 16
+    assert L.dq_grad_norm(bad, 2, 0, 0x40, None, None, WS["ws"], WS["bytes"], None) == want
+    assert L.dq_grad_clip(bad, 2, _clip(dq), None, WS["ws"], WS["bytes"], None) == want
+    assert L.dq_grad_clip(good, 2, _clip(dq), bad, WS["ws"], WS["bytes"], None) == want
+    assert L.dq_grad_gather(bad, 2, _clip(dq), flat, WS["ws"], WS["bytes"], None) == want
+    assert L.dq_grad_gather(bad, 2, None, flat, None, 0, None) == want
+    assert L.dq_grad_scatter(flat, _clip(dq), bad, 2, WS["ws"], WS["bytes"], None) == want
+    assert L.dq_grad_workspace_bytes(bad, 2, 0) == 0
+    assert L.dq_launch_count() == before
+
+
+def test_bad_arguments_are_refused(dq):
+    L = dq.lib()
+    before = L.dq_launch_count()
+    one = _list(dq, _t(dq))
+    norm = lambda *a: L.dq_grad_norm(*a, WS["ws"], WS["bytes"], None)                            # noqa: E731
+    assert norm(None, 1, 0, 0x40, None, None) == INVALID
+    assert norm(one, 1, 2, 0x40, None, None) == INVALID                                         # kind
+    assert norm(one, 1, 0, None, None, None) == INVALID                                         # no place for the norm
+    assert norm(one, 1, 0, 0x42, None, None) == ALIGNMENT
+    assert norm(one, 1, 0, 0x40, 0x42, None) == ALIGNMENT
+    assert norm(one, 1, 0, 0x40, None, 0x41) == ALIGNMENT
+    assert norm(one, 65537, 0, 0x40, None, None) == UNSUPPORTED
+    assert norm(_list(dq, _t(dq, n=(1 << 34) - 4), _t(dq, n=4)), 2, 0, 0x40, None, None) == UNSUPPORTED    # together
+    clip = lambda c, out=None: L.dq_grad_clip(one, 1, c, out, WS["ws"], WS["bytes"], None)      # noqa: E731
+    assert clip(None) == INVALID
+    assert clip(_clip(dq, -1.0)) == INVALID
+    assert clip(_clip(dq, float("nan"))) == INVALID
+    assert clip(_clip(dq, kind=7)) == INVALID
+    assert clip(_clip(dq, norm=0x82)) == ALIGNMENT
+    assert clip(_clip(dq, out_norm=0x42)) == ALIGNMENT
+    assert clip(_clip(dq), _list(dq, _t(dq, data=BASE << 8, n=MANY - 1))) == INVALID            # another size
+    a, b = _list(dq, _t(dq, row=1024, stride=2048)), _list(dq, _t(dq, data=BASE << 8, row=512, stride=2048))
+    assert L.dq_grad_clip(a, 1, _clip(dq), b, WS["ws"], WS["bytes"], None) == UNSUPPORTED       # rows of two lengths
+    for ws, size, want in ((None, 1 << 30, INVALID), (0x200, 16, INVALID), (0x208, 1 << 30, ALIGNMENT)):
+        assert L.dq_grad_norm(one, 1, 0, 0x40, None, None, ws, size, None) == want
+        assert L.dq_grad_clip(one, 1, _clip(dq), None, ws, size, None) == want
+        assert L.dq_grad_gather(one, 1, _clip(dq), BASE << 8, ws, size, None) == want
+        assert L.dq_grad_scatter(BASE << 8, _clip(dq), one, 1, ws, size, None) == want
+    assert L.dq_grad_gather(one, 1, None, None, None, 0, None) == INVALID
+    assert L.dq_grad_gather(one, 1, None, (BASE << 8) + 4, None, 0, None) == ALIGNMENT
+    assert L.dq_grad_scatter(None, None, one, 1, None, 0, None) == INVALID
+    assert L.dq_grad_scatter((BASE << 8) + 8, None, one, 1, None, 0, None) == ALIGNMENT
+    assert L.dq_launch_count() == before
+
+
+def _clip_status(dq, tensors, out=None, clip=None):
+    """The status of a call whose only fault can be an overlap: a workspace that is too small is found after it."""
+    L = dq.lib()
+    a = _list(dq, *tensors)
+    return L.dq_grad_clip(a, len(tensors), clip or _clip(dq), None if out is None else _list(dq, *out), 0x208, 1 << 30, None)
+
+
+NO_OVERLAP = ALIGNMENT              # of the workspace, which is checked last
+
+
+def test_tensors_that_overlap_are_refused(dq):
+    t = lambda at, n=MANY, **kw: _t(dq, data=BASE + at, n=n, **kw)                               # noqa: E731
+    size = 4 * MANY
+    far = 1 << 30
+    assert _clip_status(dq, [t(0), t(size)]) == NO_OVERLAP
+    assert _clip_status(dq, [t(size), t(0)]) == NO_OVERLAP
+    assert _clip_status(dq, [t(0), t(0)]) == INVALID                                             # the same one twice
+    assert _clip_status(dq, [t(0), t(size), t(size - 4)]) == INVALID
+    assert _clip_status(dq, [t(0, n=0), t(0), t(64, n=0)]) == NO_OVERLAP                         # empty ones overlap nothing
+    assert _clip_status(dq, [t(0), t(64, n=16)]) == INVALID                                      # one inside another
+    # inputs may overlap each other, outputs nothing
+    assert _clip_status(dq, [t(0), t(0)], [t(far), t(far + size)]) == NO_OVERLAP
+    assert _clip_status(dq, [t(0), t(0)], [t(far), t(far)]) == INVALID
+    assert _clip_status(dq, [t(0)], [t(size - 4)]) == INVALID
+    assert _clip_status(dq, [t(0)], [t(0)]) == INVALID
+    # an input that reaches over two outputs behind it
+    assert _clip_status(dq, [t(0, n=4 * MANY), t(far)], [t(8 * size, n=4 * MANY), t(size)]) == INVALID
+    # column blocks of one matrix lie side by side; one that is a column too wide does not
+    block = lambda col, row=1024, stride=3000: t(4 * col, row=row, stride=stride)               # noqa: E731
+    assert _clip_status(dq, [block(0), block(1024), block(2048, row=512)]) == NO_OVERLAP
+    assert _clip_status(dq, [block(0), block(1023)]) == INVALID
+    assert _clip_status(dq, [block(1024), block(0, row=2048)]) == INVALID
+    assert _clip_status(dq, [block(0), block(2048)]) == INVALID                                  # into the next row
+    assert _clip_status(dq, [block(0), block(1024, stride=4096)]) == INVALID                     # interleaved otherwise
+    # the words of the norm
+    assert _clip_status(dq, [t(0)], clip=_clip(dq, out_norm=BASE + 64)) == INVALID
+    assert _clip_status(dq, [t(0)], clip=_clip(dq, status=BASE + size - 4)) == INVALID
+    assert _clip_status(dq, [t(0)], clip=_clip(dq, out_norm=0x40, status=0x40)) == INVALID
+    assert _clip_status(dq, [t(0)], clip=_clip(dq, norm=BASE, out_norm=0x40)) == INVALID         # clipped by itself
+    assert _clip_status(dq, [t(0)], clip=_clip(dq, norm=0x40, out_norm=0x40)) == INVALID
+    L = dq.lib()
+    flat = _list(dq, t(0), t(size))
+    for at in (0, 4 * (MANY - 4), size, 2 * size - 16):
+        assert L.dq_grad_gather(flat, 2, None, BASE + at, None, 0, None) == INVALID
+        assert L.dq_grad_scatter(BASE + at, None, flat, 2, None, 0, None) == INVALID
+
+
+def test_workspace_sizes(dq):
+    L = dq.lib()
+    short, long = _list(dq, _t(dq, n=4096)), _list(dq, _t(dq))
+    assert L.dq_grad_workspace_bytes(short, 1, 0) == 0
+    assert L.dq_grad_workspace_bytes(short, 1, 1) > 0
+    assert L.dq_grad_workspace_bytes(long, 1, 0) > 0
+    assert L.dq_grad_workspace_bytes(None, 0, 0) == 0
+    many = (dq.DqTensor * 5000)(*[_t(dq, n=7)] * 5000)
+    assert L.dq_grad_workspace_bytes(many, 5000, 0) > L.dq_grad_workspace_bytes(long, 1, 0)
+
+
+class _Stream:
+    cuda_stream = 0
+
+
+def test_the_binding_refuses_what_is_no_list_of_gradients(dq):
+    cpu, out = torch.zeros(8), torch.zeros(1)
+    for bad in ([cpu], [None], [3.0], cpu, 7):
+        for call in (lambda: dq.grad_norm(bad, out_norm=out, stream=_Stream),
+                     lambda: dq.grad_clip(bad, 1.0, out_norm=out, stream=_Stream),
+                     lambda: dq.grad_gather(bad, cpu, stream=_Stream),
+                     lambda: dq.grad_scatter(cpu, bad, stream=_Stream)):
+            with pytest.raises(TypeError):
+                call()
+    for call in (lambda: dq.grad_norm([]), lambda: dq.grad_clip([], 1.0), lambda: dq.grad_gather([])):
+        with pytest.raises(ValueError, match="empty"):
+            call()
+
+
+# Fake tensors stand in for CUDA tensors; their addresses are never asked for.
+_FAKES = """
+import sys
+sys.path.insert(0, sys.argv[1])
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+import paper_1904_01197_b200 as dq
+
+class Stream:
+    cuda_stream = 0
+
+def refused(name, kind, call):
+    try:
+        call()
+    except kind as e:
+        print(name, "refused")
+        return
+    print(name, "accepted")
+
+with FakeTensorMode(allow_non_fake_inputs=True):
+    def new(*shape, dtype=torch.float32, device="cuda:0"):
+        return torch.empty(*shape, dtype=dtype, device=device)
+    f32, one, other = new(64, 64), new(1), new(64, 64, device="cuda:1")
+    S = dict(stream=Stream)
+    refused("int", TypeError, lambda: dq.grad_norm([new(8, dtype=torch.int32)], out_norm=one, **S))
+    refused("double", TypeError, lambda: dq.grad_norm([new(8, dtype=torch.float64)], out_norm=one, **S))
+    refused("sparse", TypeError, lambda: dq.grad_norm([torch.sparse_coo_tensor(size=(4, 4), device="cuda:0")], out_norm=one, **S))
+    def body(t):
+        try:
+            dq.grad_norm([t], out_norm=one, **S)
+        except RuntimeError as e:
+            print("vmap raised", "storage" in str(e))
+        return t
+    torch.vmap(body)(f32)
+"""
+
+
+def test_the_binding_refuses_other_kinds_of_tensors(dq):
+    r = subprocess.run([sys.executable, "-c", _FAKES, str(Path(__file__).resolve().parent.parent)], capture_output=True,
+                       text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    lines = r.stdout.split("\n")
+    assert lines[:3] == ["int refused", "double refused", "sparse refused"], r.stdout
+    assert "vmap raised True" in lines, r.stdout
