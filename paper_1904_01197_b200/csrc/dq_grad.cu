@@ -16,22 +16,33 @@ static_assert((int)dq::kGradF32 == DQ_F32 && (int)dq::kGradBF16 == DQ_BF16 && (i
 
 namespace {
 
-using dq::GradEntry;
-using dq::GradTable;
+// Tables of three sizes: a launch passes them by value, and every KB of parameters costs it 0.08 us.  A tensor takes 16
+// bytes of the norm's table and 24 of the other one.
+template <int W> constexpr int kSmall = 16;
+template <int W> constexpr int kMiddle = 256;
+template <int W> constexpr int kLarge = W == 3 ? 2040 : 1360;
+constexpr int kNorm = 3, kScale = 5;             // words of an entry
+static_assert(sizeof(dq::GradTable<kLarge<kNorm>, kNorm>) + 8 <= 32764, "kernel parameters");
+static_assert(sizeof(dq::GradTable<kLarge<kScale>, kScale>) + sizeof(dq::ClipArgs) <= 32764, "kernel parameters");
+constexpr int kEachMiddle = 512, kEachLarge = 8000;          // tables of the single tensors' slots, 4 bytes each
+static_assert(sizeof(dq::GradEachTable<kEachLarge>) + 64 <= 32764, "kernel parameters");
 
-// Tables of three sizes: a launch passes them by value, and 32 KB more of parameters cost it about a microsecond.
-constexpr int kSmall = 16, kMiddle = 160, kLarge = 620;
-static_assert(sizeof(GradTable<kLarge>) + sizeof(dq::ClipArgs) <= 32764, "kernel parameters");
-static_assert(sizeof(dq::GradEachTable) + 16 <= 32764, "kernel parameters");
-
-// Lists up to this many elements (and kMiddle tensors) are done by one cluster in one launch.
+// Lists up to this many elements (and half of kMiddle tensors) are done by one cluster in one launch.
 constexpr uint64_t kShortElements = 1ull << 19;
 
 // Parts of the norm: at most kMaxGrid of a launch, or one per tile where each tensor's norm is wanted as well.
-constexpr uint32_t kMaxGrid = 2048u;
-constexpr uint64_t kEachTiles = 16384u;
+constexpr uint32_t kMaxGrid = 1024u;
+constexpr uint64_t kEachTiles = 16384u;          // of full length
 
-uint32_t element_size(uint32_t dtype) { return dtype == DQ_F32 ? 4u : 2u; }
+uint32_t size_log2(uint32_t dtype) { return dtype == DQ_F32 ? 2u : 1u; }
+uint32_t element_size(uint32_t dtype) { return 1u << size_log2(dtype); }
+
+uint64_t bytes_of(const dq_tensor* list, uint32_t count)
+{
+    uint64_t bytes = 0u;
+    for (uint32_t i = 0; i < count; ++i) bytes += list[i].n << size_log2(list[i].dtype);
+    return bytes;
+}
 
 bool has_rows(const dq_tensor& t) { return t.row != 0u && t.row_stride != t.row && t.row != t.n; }
 
@@ -41,7 +52,8 @@ dq_status check_tensor(const dq_tensor& t)
     if (t.n == 0u) return DQ_OK;
     if (!t.data) return DQ_ERR_INVALID_ARG;
     if (t.n >= (1ull << 34)) return DQ_ERR_UNSUPPORTED;
-    if (reinterpret_cast<uintptr_t>(t.data) % element_size(t.dtype) != 0u) return DQ_ERR_ALIGNMENT;
+    if ((reinterpret_cast<uintptr_t>(t.data) & (element_size(t.dtype) - 1u)) != 0u) return DQ_ERR_ALIGNMENT;
+    if (reinterpret_cast<uintptr_t>(t.data) >> 57) return DQ_ERR_UNSUPPORTED;           // (no device address is as large)
     if (t.row != 0u) {
         if (t.n % t.row != 0u || t.row_stride < t.row) return DQ_ERR_INVALID_ARG;
         if (has_rows(t) && (t.row >= (1ull << 31) || t.row_stride >= (1ull << 32))) return DQ_ERR_UNSUPPORTED;
@@ -142,95 +154,160 @@ dq_status check_outputs(const dq_tensor* in, uint32_t in_count, const dq_tensor*
 }
 
 // ------------------------------------------------------------------------------------------ tables
-// The walk of one tensor.  src alone: `dst` null.
-GradEntry entry_of(const dq_tensor& src, const dq_tensor* dst)
+// Rows that are not Wide and at least this long are walked one by one; shorter ones element by element.
+constexpr uint64_t kLongRow = 256u;
+
+// How a tensor is walked, and how many elements before the first one its tiles begin: where the destination (the source,
+// where there is none) is aligned.
+struct Walk {
+    uint32_t walk, phase;
+    uint64_t row, src_stride, dst_stride;
+};
+
+Walk walk_of(const dq_tensor& src, const dq_tensor* dst)
 {
-    GradEntry e = {};
     const dq_tensor& to = dst ? *dst : src;
     const uint32_t ss = element_size(src.dtype), ds = element_size(to.dtype);
     const uintptr_t s = reinterpret_cast<uintptr_t>(src.data), d = reinterpret_cast<uintptr_t>(to.data);
-    e.src = src.data;
-    e.dst = to.data;
-    e.n = src.n;
-    if (!has_rows(src) && !has_rows(to)) {
-        // groups begin where the destination (the source, where there is none) is aligned
-        const uint32_t phase = (uint32_t)(d / ds % (16u / ds));
-        const uint32_t shift = (uint32_t)((s - phase * ss) & 15u);
-        e.form = dq::grad_form(src.dtype, to.dtype, dq::kGradFlat, phase, shift);
-        return e;
-    }
-    e.row = (uint32_t)(has_rows(src) ? src.row : to.row);
-    e.src_stride = has_rows(src) ? (uint32_t)src.row_stride : e.row;
-    e.dst_stride = has_rows(to) ? (uint32_t)to.row_stride : e.row;
-    const bool wide = e.row % 8u == 0u && ((s | d) & 15u) == 0u && (uint64_t)e.src_stride * ss % 16u == 0u &&
-                      (uint64_t)e.dst_stride * ds % 16u == 0u;
-    e.form = dq::grad_form(src.dtype, to.dtype, wide ? dq::kGradRows : dq::kGradLoose, 0u, 0u);
-    return e;
+    if (!has_rows(src) && !has_rows(to)) return {dq::kGradFlat, (uint32_t)(d & 15u) >> size_log2(to.dtype), 0u, 0u, 0u};
+    Walk w = {dq::kGradLoose, 0u, has_rows(src) ? src.row : to.row, 0u, 0u};
+    w.src_stride = has_rows(src) ? src.row_stride : w.row;
+    w.dst_stride = has_rows(to) ? to.row_stride : w.row;
+    if (w.row % 8u == 0u && ((s | d) & 15u) == 0u && w.src_stride * ss % 16u == 0u && w.dst_stride * ds % 16u == 0u)
+        w.walk = dq::kGradWide;
+    else if (w.row >= kLongRow)
+        w.walk = dq::kGradLong;
+    return w;
 }
 
-uint32_t tiles_of(const GradEntry& e, uint32_t tile_log2)
+uint32_t tiles_of(uint64_t n, const Walk& w, uint32_t tile_len)
 {
-    return (uint32_t)((e.n + ((e.form >> 8) & 15u) + (1ull << tile_log2) - 1u) >> tile_log2);
+    if (w.walk == dq::kGradLong) return (uint32_t)dq::GradRowTiles((uint32_t)w.row, tile_len).tiles(n / w.row);
+    return (uint32_t)((n + w.phase + tile_len - 1u) / tile_len);
 }
 
-// Fills a table from list position *next on; first[i], where given, is the first slot of tensor i.
-template <int N>
-void fill(GradTable<N>& t, const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_log2, uint32_t* next)
+uint32_t step_up(uint64_t len)
+{
+    return (uint32_t)std::max<uint64_t>(1u, (len + dq::kGradTileStep - 1u) / dq::kGradTileStep) * dq::kGradTileStep;
+}
+
+// The tiles of the norm's kernel, which runs in one wave: 8 KB, two batches of 16-byte loads of a lane, but 1024 elements where
+// that leaves warps without a tile, and more where a warp has more than four of them, which costs it look-ups (n = 124 M
+// bf16: 2048 to 16384 elements 40 us; 25.6 M fp32: 2048 19.8 us, 4096 20.8, 1024 21.5; 25.6 M bf16: 4096 13.7, 2048 14.9; 1.7 M
+// fp32: 1024 4.1, 2048 4.4).
+uint32_t norm_tile_length(uint64_t total, uint64_t bytes, int sms)
+{
+    const uint64_t warps = (uint64_t)sms * dq::kGradNormCtas * dq::kGradWarps;
+    if (total < warps * 1024u) return 1024u;
+    const uint64_t tile = bytes < 3u * total ? 4096u : 2048u;
+    return (uint32_t)(tile * (total / (warps * tile * 4u) + 1u));
+}
+
+// The tiles of the kernel that scales.  Up to two tiles of 4096 per resident warp it runs in one wave or little more, since every
+// CTA begins with the parts of the norm; longer lists run in many short CTAs, which the hardware hands out as others end: 124 M
+// fp32 elements 149 us, in one wave of long CTAs 166 (11.7 M: 4096 elements 21.5 us, 2048 23.0; 1.7 M: 1024 7.0 us, 4096 9.0).
+uint32_t scale_tile_length(uint64_t total, int sms)
+{
+    const uint64_t warps = (uint64_t)sms * dq::kGradScaleCtas * dq::kGradWarps;
+    return total < warps * 8192u ? std::min(4096u, step_up(total / warps + 1u)) : 2048u;
+}
+constexpr uint32_t kScaleGrid = 24u;             // CTAs per SM of a launch, resident or not
+
+// The tiles of a cluster: one per warp.
+uint32_t cluster_tile_length(uint64_t total, uint32_t count)
+{
+    const uint32_t warps = dq::kGradCluster * dq::kGradClusterThreads / 32u;
+    return step_up(total / (warps - std::min(count, warps / 2u)) + 1u);
+}
+
+// What the norm's pass leaves in L2 for the pass that scales, which begins at the end: more than this is read with the policy
+// to go first (n = 124 M fp32, 64 MB: 229 us; all kept: 232, none: 237, and with ordinary stores 242).
+constexpr uint64_t kKeepBytes = 64ull << 20;
+
+uint32_t entries_of(const dq_tensor& src, const dq_tensor* dst)
+{
+    return src.n == 0u ? 0u : has_rows(src) || (dst && has_rows(*dst)) ? 2u : 1u;
+}
+
+// Fills a table from list position *next on.
+template <int N, int W>
+void fill(dq::GradTable<N, W>& t, const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next)
 {
     t.count = 0u;
-    t.tile_log2 = tile_log2;
+    t.tile_len = tile_len;
+    t.stream_below = t.rows = 0u;
     uint32_t tiles = 0u;
-    while (*next < count && t.count < (uint32_t)N) {
-        const uint32_t i = (*next)++;
-        if (src[i].n == 0u) continue;
-        const GradEntry e = entry_of(src[i], dst ? dst + i : nullptr);
-        t.first_tile[t.count] = tiles;
-        t.e[t.count++] = e;
-        tiles += tiles_of(e, tile_log2);
+    for (; *next < count; ++*next) {
+        const uint32_t i = *next;
+        const dq_tensor* to = dst ? dst + i : nullptr;
+        const uint32_t entries = entries_of(src[i], to);
+        if (entries == 0u) continue;
+        if (t.count + entries > (uint32_t)N) break;
+        const Walk w = walk_of(src[i], to);
+        const uint64_t s = reinterpret_cast<uintptr_t>(src[i].data), n = src[i].n;
+        dq::GradEntry<W>& e = t.e[t.count];
+        t.first_tile[t.count++] = tiles;
+        tiles += tiles_of(n, w, tile_len);
+        e.w[0] = (uint32_t)s;
+        e.w[1] = (uint32_t)(s >> 32) | (uint32_t)src[i].dtype << 25 | w.walk << 27 | (uint32_t)(n >> 32) << 29;
+        e.w[2] = (uint32_t)n;
+        if constexpr (W > 3) {
+            const uint64_t d = reinterpret_cast<uintptr_t>(to->data);
+            e.w[3] = (uint32_t)d;
+            e.w[4] = (uint32_t)(d >> 32) | (uint32_t)to->dtype << 25;
+        }
+        if (entries == 2u) {
+            t.rows = 1u;
+            dq::GradEntry<W>& rows = t.e[t.count];
+            t.first_tile[t.count++] = tiles;
+            rows.w[0] = (uint32_t)w.row;
+            rows.w[1] = (uint32_t)w.src_stride;
+            rows.w[2] = (uint32_t)w.dst_stride;
+        }
     }
     t.first_tile[t.count] = tiles;
 }
 
-uint32_t grid_for(uint32_t tiles, int sms, uint32_t ctas_per_sm)
+uint32_t grid_for(uint32_t tiles, uint32_t warps, uint32_t most)
 {
-    const uint32_t most = std::min((uint32_t)sms * ctas_per_sm, kMaxGrid);
-    return std::max(1u, std::min((tiles + dq::kGradWarps - 1u) / dq::kGradWarps, most));
+    return std::max(1u, std::min((tiles + warps - 1u) / warps, most));
+}
+
+uint64_t entries_in(const dq_tensor* src, const dq_tensor* dst, uint32_t count)
+{
+    uint64_t entries = 0u;
+    for (uint32_t i = 0; i < count; ++i) entries += entries_of(src[i], dst ? dst + i : nullptr);
+    return entries;
 }
 
 // Calls f(table) with the smallest table that holds the rest of the list.
-template <class F>
-cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_log2, uint32_t* next, F&& f)
+template <int W, class F>
+cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next, F&& f)
 {
-    uint32_t left = 0u;
-    for (uint32_t i = *next; i < count && left <= (uint32_t)kMiddle; ++i) left += src[i].n != 0u;
-    if (left <= (uint32_t)kSmall) {
-        GradTable<kSmall> t;
-        fill(t, src, dst, count, tile_log2, next);
+    const uint64_t left = entries_in(src + *next, dst ? dst + *next : nullptr, count - *next);
+    if (left <= (uint64_t)kSmall<W>) {
+        dq::GradTable<kSmall<W>, W> t;
+        fill(t, src, dst, count, tile_len, next);
         return f(t);
     }
-    if (left <= (uint32_t)kMiddle) {
-        GradTable<kMiddle> t;
-        fill(t, src, dst, count, tile_log2, next);
+    if (left <= (uint64_t)kMiddle<W>) {
+        dq::GradTable<kMiddle<W>, W> t;
+        fill(t, src, dst, count, tile_len, next);
         return f(t);
     }
-    GradTable<kLarge> t;
-    fill(t, src, dst, count, tile_log2, next);
+    dq::GradTable<kLarge<W>, W> t;
+    fill(t, src, dst, count, tile_len, next);
     return f(t);
 }
 
-bool is_short(const dq_tensor* list, uint32_t count, uint64_t total)
-{
-    if (total > kShortElements) return false;
-    uint32_t tensors = 0u;
-    for (uint32_t i = 0; i < count; ++i) tensors += list[i].n != 0u;
-    return tensors <= (uint32_t)kMiddle;
-}
+// A list that one cluster does in one launch.  (A tensor in rows on either side takes two entries of the table.)
+bool is_short(uint32_t count, uint64_t total) { return total <= kShortElements && 2u * (uint64_t)count <= (uint64_t)kMiddle<kScale>; }
 
 constexpr int kMaxDevices = 64;
 
 // CTAs of the cluster kernels: 16 (which needs an attribute per kernel and device) where one can be resident, else the
 // portable 8; 0 on a CUDA error.
-template <class Table, bool MAX, bool SCALE>
+template <class Table, bool ROWS, bool MAX, bool SCALE>
 uint32_t cluster_size()
 {
     static std::mutex mu;
@@ -239,7 +316,7 @@ uint32_t cluster_size()
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0u;
     std::lock_guard<std::mutex> lock(mu);
     if (size[dev] == 0u) {
-        auto kernel = dq::grad_cluster_kernel<Table, MAX, SCALE>;
+        auto kernel = dq::grad_cluster_kernel<Table, ROWS, MAX, SCALE>;
         uint32_t s = 8u;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
@@ -262,35 +339,44 @@ uint32_t cluster_size()
     return size[dev];
 }
 
-template <bool MAX, bool SCALE, class Table>
-cudaError_t launch_cluster(const Table& t, const dq::ClipArgs& a, cudaStream_t st)
+template <bool ROWS, bool MAX, bool SCALE, class Table>
+cudaError_t launch_cluster_of(const Table& t, const dq::ClipArgs& a, cudaStream_t st)
 {
-    const uint32_t most = cluster_size<Table, MAX, SCALE>();
+    const uint32_t most = cluster_size<Table, ROWS, MAX, SCALE>();
     if (most == 0u) return cudaErrorUnknown;
     // no CTA without a tile for every other warp
     const uint32_t tiles = t.first_tile[t.count];
     uint32_t ctas = 1u;
     while (ctas < most && tiles > ctas * (dq::kGradClusterThreads / 64u)) ctas *= 2u;
-    const cudaError_t e = dq::launch_overlapped(dq::grad_cluster_kernel<Table, MAX, SCALE>, ctas,
+    const cudaError_t e = dq::launch_overlapped(dq::grad_cluster_kernel<Table, ROWS, MAX, SCALE>, ctas,
                                                 (uint32_t)dq::kGradClusterThreads, 0, st, ctas, t, a);
     if (e == cudaSuccess) dq::count_launch();
     return e;
 }
 
+template <bool MAX, bool SCALE, class Table>
+cudaError_t launch_cluster(const Table& t, const dq::ClipArgs& a, cudaStream_t st)
+{
+    return t.rows ? launch_cluster_of<true, MAX, SCALE>(t, a, st) : launch_cluster_of<false, MAX, SCALE>(t, a, st);
+}
+
 // The parts of the norm of a list into slots; *num_slots counts them.
 template <bool MAX, bool EACH>
-cudaError_t launch_parts(const dq_tensor* list, uint32_t count, uint32_t tile_log2, int sms, dq::NormPart<MAX>* slots,
-                         uint32_t* num_slots, cudaStream_t st)
+cudaError_t launch_parts(const dq_tensor* list, uint32_t count, uint32_t tile_len, int sms, uint64_t keep,
+                         dq::NormPart<MAX>* slots, uint32_t* num_slots, cudaStream_t st)
 {
     *num_slots = 0u;
     for (uint32_t next = 0u; next < count;) {
-        const cudaError_t e = with_table(list, nullptr, count, tile_log2, &next, [&](const auto& t) {
-            using Table = std::remove_cv_t<std::remove_reference_t<decltype(t)>>;
+        const cudaError_t e = with_table<kNorm>(list, nullptr, count, tile_len, &next, [&](auto& t) {
+            using Table = std::remove_reference_t<decltype(t)>;
             const uint32_t tiles = t.first_tile[t.count];
             if (tiles == 0u) return cudaSuccess;
-            const uint32_t grid = grid_for(tiles, sms, 8u);
-            const cudaError_t r = dq::launch_overlapped(dq::grad_norm_kernel<Table, MAX, EACH>, grid,
-                                                        (uint32_t)dq::kGradThreads, 0, st, 1u, t, slots + *num_slots);
+            const uint64_t kept = keep / tile_len;
+            t.stream_below = tiles > kept ? (uint32_t)(tiles - kept) : 0u;
+            const uint32_t grid = grid_for(tiles, dq::kGradWarps, std::min((uint32_t)sms * dq::kGradNormCtas, kMaxGrid));
+            const cudaError_t r = dq::launch_overlapped(t.rows ? dq::grad_norm_kernel<Table, true, MAX, EACH>
+                                                               : dq::grad_norm_kernel<Table, false, MAX, EACH>,
+                                                        grid, (uint32_t)dq::kGradThreads, 0, st, 1u, t, slots + *num_slots);
             if (r == cudaSuccess) dq::count_launch();
             *num_slots += EACH ? tiles : grid;
             return r;
@@ -300,37 +386,54 @@ cudaError_t launch_parts(const dq_tensor* list, uint32_t count, uint32_t tile_lo
     return cudaSuccess;
 }
 
-template <bool MAX>
-cudaError_t launch_join(const dq::NormPart<MAX>* slots, uint32_t num_slots, float* out_norm, uint32_t* status, cudaStream_t st)
+// The whole from its parts, and with a table the norms of its tensors.
+template <bool MAX, class Table>
+cudaError_t launch_join(const Table& t, const dq::NormPart<MAX>* slots, uint32_t num_slots, float* out_norm, float* out_norms,
+                        uint32_t* status, cudaStream_t st)
 {
-    const cudaError_t e = dq::launch_overlapped(dq::grad_norm_join_kernel<MAX>, 1u, (uint32_t)dq::kGradJoinThreads, 0, st, 1u,
-                                                slots, num_slots, out_norm, status);
+    constexpr uint32_t kPerCta = dq::kGradJoinThreads / 32;
+    const cudaError_t e = dq::launch_overlapped(dq::grad_norm_join_kernel<Table, MAX>, 1u + (t.count + kPerCta - 1u) / kPerCta,
+                                                (uint32_t)dq::kGradJoinThreads, 0, st, 1u, t, slots, num_slots, out_norm,
+                                                out_norms, status);
     if (e == cudaSuccess) dq::count_launch();
     return e;
 }
 
-// The norms of single tensors, after launch_parts<MAX, true>.
 template <bool MAX>
-cudaError_t launch_each(const dq_tensor* list, uint32_t count, uint32_t tile_log2, const dq::NormPart<MAX>* slots,
-                        float* out_norms, cudaStream_t st)
+cudaError_t launch_join(const dq::NormPart<MAX>* slots, uint32_t num_slots, float* out_norm, uint32_t* status, cudaStream_t st)
 {
-    uint32_t slot = 0u;
-    for (uint32_t i = 0u; i < count;) {
-        dq::GradEachTable t;
+    dq::GradEachTable<1> none;
+    none.count = 0u;
+    return launch_join<MAX>(none, slots, num_slots, out_norm, nullptr, status, st);
+}
+
+// The same with the norms of single tensors, after launch_parts<MAX, true>.
+template <bool MAX>
+cudaError_t launch_join_each(const dq_tensor* list, uint32_t count, uint32_t tile_len, const dq::NormPart<MAX>* slots,
+                             uint32_t num_slots, float* out_norm, float* out_norms, uint32_t* status, cudaStream_t st)
+{
+    uint32_t slot = 0u, i = 0u;
+    auto launch = [&](auto& t) {
         const uint32_t begin = i;
         t.count = 0u;
         t.first[0] = slot;
-        for (; i < count && t.count < (uint32_t)dq::kGradEachCapacity; ++i) {
-            if (list[i].n) slot += tiles_of(entry_of(list[i], nullptr), tile_log2);
+        for (; i < count && t.count < (uint32_t)t.kCapacity; ++i) {
+            if (list[i].n) slot += tiles_of(list[i].n, walk_of(list[i], nullptr), tile_len);
             t.first[++t.count] = slot;
         }
-        const cudaError_t e = dq::launch_overlapped(dq::grad_norms_each_kernel<MAX>,
-                                                    (t.count + dq::kGradWarps - 1u) / dq::kGradWarps,
-                                                    (uint32_t)dq::kGradThreads, 0, st, 1u, t, slots, out_norms + begin);
-        if (e != cudaSuccess) return e;
-        dq::count_launch();
+        return launch_join<MAX>(t, slots, num_slots, begin == 0u ? out_norm : nullptr, out_norms + begin, status, st);
+    };
+    cudaError_t e = cudaSuccess;
+    while (i < count && e == cudaSuccess) {
+        if (count - i <= (uint32_t)kEachMiddle) {
+            dq::GradEachTable<kEachMiddle> t;
+            e = launch(t);
+        } else {
+            dq::GradEachTable<kEachLarge> t;
+            e = launch(t);
+        }
     }
-    return cudaSuccess;
+    return e;
 }
 
 template <bool MAX>
@@ -340,22 +443,24 @@ dq_status norm_of(const dq_tensor* list, uint32_t count, uint64_t total, float* 
     const int sms = dq::device_sm_count();
     if (sms <= 0) return DQ_ERR_CUDA;
     auto* slots = static_cast<dq::NormPart<MAX>*>(workspace);
-    uint32_t num_slots = 0u, tile_log2 = dq::kGradTileLog2;
+    const uint64_t bytes = bytes_of(list, count);
+    uint32_t num_slots = 0u;
     cudaError_t e;
     if (out_norms && count) {
-        while ((total >> tile_log2) > kEachTiles) ++tile_log2;
-        e = launch_parts<MAX, true>(list, count, tile_log2, sms, slots, &num_slots, st);
-        if (e == cudaSuccess) e = launch_each<MAX>(list, count, tile_log2, slots, out_norms, st);
-        if (e == cudaSuccess) e = launch_join<MAX>(slots, num_slots, out_norm, status, st);
-    } else if (is_short(list, count, total)) {
+        // (no more slots than the workspace has)
+        const uint32_t tile_len = std::max(norm_tile_length(total, bytes, sms), step_up(total / kEachTiles + 1u));
+        e = launch_parts<MAX, true>(list, count, tile_len, sms, ~0ull, slots, &num_slots, st);
+        if (e == cudaSuccess)
+            e = launch_join_each<MAX>(list, count, tile_len, slots, num_slots, out_norm, out_norms, status, st);
+    } else if (is_short(count, total)) {
         dq::ClipArgs a = {};
         a.out_norm = out_norm;
         a.status = status;
         uint32_t next = 0u;
-        e = with_table(list, nullptr, count, tile_log2, &next,
-                       [&](const auto& t) { return launch_cluster<MAX, false>(t, a, st); });
+        e = with_table<kNorm>(list, nullptr, count, cluster_tile_length(total, count), &next,
+                              [&](const auto& t) { return launch_cluster<MAX, false>(t, a, st); });
     } else {
-        e = launch_parts<MAX, false>(list, count, tile_log2, sms, slots, &num_slots, st);
+        e = launch_parts<MAX, false>(list, count, norm_tile_length(total, bytes, sms), sms, ~0ull, slots, &num_slots, st);
         if (e == cudaSuccess) e = launch_join<MAX>(slots, num_slots, out_norm, status, st);
     }
     return e == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
@@ -370,26 +475,28 @@ dq_status scale(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint
     if (sms <= 0) return DQ_ERR_CUDA;
     dq::ClipArgs a = {};
     a.in_place = in_place ? 1u : 0u;
+    a.max_kind = MAX ? 1u : 0u;
+    a.stream = 1u;
     a.max_norm = clip ? clip->max_norm : 0.0f;
-    uint32_t next = 0u, tile_log2 = dq::kGradTileLog2;
+    uint32_t next = 0u;
     if (clip) {
         a.norm = clip->norm;
         a.out_norm = clip->out_norm;
         a.status = clip->status_word;
     }
     if (clip && !clip->norm) {
-        if (is_short(src, count, total)) {
-            const cudaError_t e = with_table(src, dst, count, tile_log2, &next,
-                                             [&](const auto& t) { return launch_cluster<MAX, true>(t, a, st); });
+        if (is_short(count, total)) {
+            const cudaError_t e = with_table<kScale>(src, dst, count, cluster_tile_length(total, count), &next,
+                                                     [&](const auto& t) { return launch_cluster<MAX, true>(t, a, st); });
             return e == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
         }
         auto* slots = reinterpret_cast<dq::NormPart<MAX>*>(static_cast<char*>(workspace) + 16);
-        cudaError_t e = launch_parts<MAX, false>(norm_list, norm_count, tile_log2, sms, slots, &a.num_slots, st);
+        const uint64_t bytes = bytes_of(norm_list, norm_count);
+        cudaError_t e = launch_parts<MAX, false>(norm_list, norm_count, norm_tile_length(total, bytes, sms), sms,
+                                                kKeepBytes * total / bytes, slots, &a.num_slots, st);
         if (e != cudaSuccess) return DQ_ERR_CUDA;
         a.slots = slots;
-        uint32_t tensors = 0u;
-        for (uint32_t i = 0; i < count; ++i) tensors += src[i].n != 0u;
-        if (tensors > (uint32_t)kLarge) {
+        if (entries_in(src, dst, count) > (uint64_t)kLarge<kScale>) {
             // several launches follow: they take the norm itself
             float* norm = a.out_norm ? a.out_norm : static_cast<float*>(workspace);
             if (launch_join<MAX>(slots, a.num_slots, norm, a.status, st) != cudaSuccess) return DQ_ERR_CUDA;
@@ -399,13 +506,15 @@ dq_status scale(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint
             a.status = nullptr;
         }
     }
+    const uint32_t tile_len = scale_tile_length(total, sms);
     bool first = true;
     while (next < count || first) {
-        const cudaError_t e = with_table(src, dst, count, tile_log2, &next, [&](const auto& t) {
+        const cudaError_t e = with_table<kScale>(src, dst, count, tile_len, &next, [&](const auto& t) {
             using Table = std::remove_cv_t<std::remove_reference_t<decltype(t)>>;
             const uint32_t tiles = t.first_tile[t.count];
             if (tiles == 0u && !(first && (a.out_norm || a.status))) return cudaSuccess;
-            const cudaError_t r = dq::launch_overlapped(dq::grad_scale_kernel<Table, MAX>, grid_for(tiles, sms, 8u),
+            const cudaError_t r = dq::launch_overlapped(t.rows ? dq::grad_scale_kernel<Table, true>
+                                                               : dq::grad_scale_kernel<Table, false>, grid_for(tiles, dq::kGradWarps, (uint32_t)sms * kScaleGrid),
                                                         (uint32_t)dq::kGradThreads, 0, st, 1u, t, a);
             if (r == cudaSuccess) dq::count_launch();
             return r;
@@ -479,9 +588,10 @@ extern "C" {
 uint64_t dq_grad_workspace_bytes(const dq_tensor* list, uint32_t count, int each)
 {
     uint64_t total;
-    if (check_list(list, count, &total) != DQ_OK || (!each && is_short(list, count, total))) return 0u;
-    const uint64_t slots = each ? kEachTiles + 2u * (uint64_t)count
-                                : (uint64_t)kMaxGrid * ((count + (uint32_t)kLarge - 1u) / (uint32_t)kLarge);
+    if (check_list(list, count, &total) != DQ_OK || (!each && is_short(count, total))) return 0u;
+    // (tiles of a tensor in rows may be half as long, and every tensor may have two that are short)
+    const uint64_t slots = each ? 2u * kEachTiles + kEachTiles / 8u + 2u * (uint64_t)count
+                                : (uint64_t)kMaxGrid * (2u * (uint64_t)count / (uint64_t)(kLarge<kNorm> - 1) + 1u);
     return (16u + 8u * slots + 255u) / 256u * 256u;
 }
 

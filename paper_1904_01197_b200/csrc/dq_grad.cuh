@@ -26,9 +26,9 @@
 namespace dq {
 
 constexpr int kGradThreads = 256;
+constexpr int kGradNormCtas = 4, kGradScaleCtas = 3;         // resident CTAs per SM: 64 and 80 registers
 constexpr uint32_t kGradWarps = kGradThreads / 32;
-constexpr uint32_t kGradBatch = 4;                           // groups of a lane in flight
-constexpr uint32_t kGradTileLog2 = 10;                       // 32 lanes * 8 elements * kGradBatch
+constexpr uint32_t kGradTileStep = 1024;                     // a warp's batch of 8 loads of 16 bytes per lane, in fp32
 constexpr int kGradClusterThreads = 512;
 constexpr int kGradCluster = 16;                             // 8 where a cluster of 16 cannot be resident
 
@@ -36,100 +36,81 @@ constexpr uint32_t kWarnNonfiniteNorm = 0x8u;      // DQ_WARN_NONFINITE_NORM
 
 enum GradType : uint32_t { kGradF32 = 0, kGradBF16 = 1, kGradF16 = 2 };
 
-// How a tensor is walked.  Flat: contiguous on both sides.  Rows: rows of contiguous elements at a fixed distance, every
-// row a multiple of 8 elements that starts at a 16-byte boundary.  Loose: rows of any other kind, element by element.
-enum GradWalk : uint32_t { kGradFlat = 0, kGradRows = 1, kGradLoose = 2 };
+// How a tensor is walked.  Flat: contiguous on both sides.  Of tensors in rows, Wide: in 16-byte pieces across the rows, which
+// are multiples of 8 elements and start at 16-byte boundaries.  Long: rows of another kind, each like a contiguous tensor of
+// its own.  Loose: element by element, where those are short.
+enum GradWalk : uint32_t { kGradFlat = 0, kGradLong = 1, kGradWide = 2, kGradLoose = 3 };
 
+// Tiles of a Long tensor: parts of a row, of nearly equal length, where a row does not fit a tile whatever its alignment,
+// else several whole rows.
+struct GradRowTiles {
+    uint32_t per_row, rows;      // tiles per row, rows per tile: one of them is 1
+    uint32_t len;                // of a part
+
+    __host__ __device__ __forceinline__ GradRowTiles(uint32_t row, uint32_t tile_len)
+        : per_row((row + 7u + tile_len - 1u) / tile_len), rows(per_row > 1u ? 1u : tile_len / row),
+          len((row + 7u + 8u * per_row - 1u) / (8u * per_row) * 8u)
+    {
+    }
+    __host__ __device__ __forceinline__ uint64_t tiles(uint64_t all_rows) const
+    {
+        return per_row > 1u ? all_rows * per_row : (all_rows + rows - 1u) / rows;
+    }
+};
+
+// A tensor in a launch's table, in as few words as hold it: addresses have at most 57 bits, lengths 34.
+//   w[0], low 25 bits of w[1]   address of the source        w[1] 25..26 type, 27..28 walk, 29..30 upper bits of n
+//   w[2]                        lower bits of n
+//   w[3], low 25 bits of w[4]   address of the destination   w[4] 25..26 type                      (where there is one)
+// A tensor in rows takes the next entry too, which owns no tiles: w[0] elements per row, w[1] from one row of the source to
+// the next, w[2] of the destination.
+template <int W>
 struct GradEntry {
-    const void* src;
-    uint64_t n;
-    uint32_t row, src_stride;        // rows: elements per row, and from one row to the next
-    uint32_t form;                   // src type | dst type << 2 | walk << 4 | phase << 8 | byte shift of the source << 12
-    uint32_t dst_stride;
-    void* dst;
+    uint32_t w[W];
 };
 
-__host__ __device__ __forceinline__ uint32_t grad_form(uint32_t src_type, uint32_t dst_type, uint32_t walk, uint32_t phase,
-                                                       uint32_t shift)
-{
-    return src_type | dst_type << 2 | walk << 4 | phase << 8 | shift << 12;
-}
-
-// first_tile[count] is the launch's number of tiles.
-template <int N>
+// first_tile[count] is the launch's number of tiles.  The tiles below stream_below are not wanted in L2 for long; rows: a
+// tensor of the table lies in rows.
+template <int N, int W>
 struct GradTable {
-    static constexpr int kCapacity = N;
-    uint32_t count, tile_log2;
+    static constexpr int kCapacity = N, kWords = W;
+    uint32_t count, tile_len, stream_below, rows;
     uint32_t first_tile[N + 1];
-    GradEntry e[N];
+    GradEntry<W> e[N];
 };
 
-// ------------------------------------------------------------------------------------------ values of a group
-__device__ __forceinline__ void widen_bf16(const uint32_t (&w)[4], float (&x)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
+// ... unpacked.
+struct GradTensor {
+    const char* src;
+    char* dst;
+    uint64_t n;
+    uint32_t src_type, dst_type, walk;
+    uint32_t row, src_stride, dst_stride;
+};
 
-__device__ __forceinline__ void widen_f16(const uint32_t (&w)[4], float (&x)[8])
+template <bool ROWS, class Table>
+__device__ __forceinline__ GradTensor tensor_at(const Table& t, uint32_t k)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
+    GradTensor g;
+    const uint32_t w1 = t.e[k].w[1];
+    g.src = reinterpret_cast<const char*>((uint64_t)(w1 & 0x1FFFFFFu) << 32 | t.e[k].w[0]);
+    g.src_type = w1 >> 25 & 3u;
+    g.walk = w1 >> 27 & 3u;
+    g.n = (uint64_t)(w1 >> 29 & 3u) << 32 | t.e[k].w[2];
+    g.dst = nullptr;
+    g.dst_type = 0u;
+    if constexpr (Table::kWords > 3) {
+        const uint32_t w4 = t.e[k].w[4];
+        g.dst = reinterpret_cast<char*>((uint64_t)(w4 & 0x1FFFFFFu) << 32 | t.e[k].w[3]);
+        g.dst_type = w4 >> 25 & 3u;
     }
-}
-
-__device__ __forceinline__ float load_element(const void* p, uint64_t i, uint32_t type)
-{
-    if (type == kGradF32) return static_cast<const float*>(p)[i];
-    const uint16_t h = static_cast<const uint16_t*>(p)[i];
-    return type == kGradBF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
-}
-
-// One rounding, of the product in fp32 to the destination's type (to nearest, ties to even).
-__device__ __forceinline__ void store_element(void* p, uint64_t i, uint32_t type, float x)
-{
-    if (type == kGradF32)
-        static_cast<float*>(p)[i] = x;
-    else if (type == kGradBF16)
-        static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
-    else
-        static_cast<__half*>(p)[i] = __float2half_rn(x);
-}
-
-// W words that start `shift` bytes into the P pieces at q: word moves by the shift's two upper bits, half a word by the
-// next (16-bit elements only).
-template <int P, int W, bool HALF>
-__device__ __forceinline__ void shifted_words(const uint4 (&q)[P], uint32_t shift, uint32_t (&out)[W])
-{
-    uint32_t w[4 * P];
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        w[4 * i] = q[i].x;
-        w[4 * i + 1] = q[i].y;
-        w[4 * i + 2] = q[i].z;
-        w[4 * i + 3] = q[i].w;
+    g.row = g.src_stride = g.dst_stride = 0u;
+    if (ROWS && g.walk != kGradFlat) {
+        g.row = t.e[k + 1u].w[0];
+        g.src_stride = t.e[k + 1u].w[1];
+        g.dst_stride = t.e[k + 1u].w[2];
     }
-    if (shift & 8u) {
-#pragma unroll
-        for (int i = 0; i + 2 < 4 * P; ++i) w[i] = w[i + 2];
-    }
-    if (shift & 4u) {
-#pragma unroll
-        for (int i = 0; i + 1 < 4 * P; ++i) w[i] = w[i + 1];
-    }
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        out[i] = w[i];
-        if constexpr (HALF) {
-            if (shift & 2u) out[i] = __funnelshift_r(w[i], w[i + 1], 16);
-        }
-    }
+    return g;
 }
 
 // ------------------------------------------------------------------------------------------ a warp's place in the table
@@ -139,175 +120,209 @@ template <class Table>
 __device__ __forceinline__ uint32_t find_tensor(const Table& t, uint32_t tile)
 {
     const uint32_t lane = threadIdx.x & 31u;
-    uint32_t block = 0u;
-    if constexpr (Table::kCapacity > 32) {
-        static_assert(Table::kCapacity <= 1024, "two steps of 32");
-        const uint32_t i = lane * 32u;
-        block = 32u * (__popc(__ballot_sync(0xFFFFFFFFu, i < t.count && t.first_tile[i < t.count ? i : 0u] <= tile)) - 1u);
+    auto at_or_before = [&](uint32_t i) {
+        const bool in = i < t.count;
+        return (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, in && t.first_tile[in ? i : 0u] <= tile));
+    };
+    if constexpr (Table::kCapacity <= 32) {
+        return at_or_before(lane) - 1u;
+    } else {
+        constexpr uint32_t kStep = (Table::kCapacity + 1023) / 1024 * 32;
+        const uint32_t block = kStep * (at_or_before(lane * kStep) - 1u);
+        uint32_t k = block - 1u;
+#pragma unroll
+        for (uint32_t i = 0u; i < kStep; i += 32u) k += at_or_before(block + i + lane);
+        return k;
     }
-    const uint32_t i = block + lane;
-    return block + __popc(__ballot_sync(0xFFFFFFFFu, i < t.count && t.first_tile[i < t.count ? i : 0u] <= tile)) - 1u;
 }
 
-// A tile's place in its tensor.
+// A warp's current tensor.
+struct TensorRun {
+    GradTensor g;
+    uint32_t first, end;         // its tiles
+
+    // Before the wait for the previous kernel: the parameters' cache misses pass in its shadow.
+    template <bool ROWS, class Table>
+    __device__ __forceinline__ void start(const Table& t, uint32_t tile, uint32_t tiles)
+    {
+        first = end = 0u;
+        if (tile < tiles) seek<ROWS>(t, tile);
+    }
+
+    template <bool ROWS, class Table>
+    __device__ __forceinline__ void seek(const Table& t, uint32_t tile)
+    {
+        const uint32_t k = find_tensor(t, tile);
+        g = tensor_at<ROWS>(t, k);
+        first = t.first_tile[k];
+        end = t.first_tile[k + 1u];
+    }
+};
+
+// How many elements before the first one a contiguous tensor's tiles begin: where the destination is aligned, or the
+// source where there is none.  (The host counts tiles by the same rule.)
+__device__ __forceinline__ uint32_t tile_phase(const GradTensor& g)
+{
+    const uint32_t size = (g.dst ? g.dst_type : g.src_type) == kGradF32 ? 4u : 2u;
+    return (uint32_t)(reinterpret_cast<uintptr_t>(g.dst ? g.dst : g.src) / size) % (16u / size);
+}
+
+// Calls work(piece, tile, tile_len) for what a tile covers.  Pieces are contiguous tensors, a row each, or the tensor itself
+// (which is contiguous unless ROWS).
+template <bool ROWS, class Work>
+__device__ __forceinline__ void for_pieces(const GradTensor& g, uint32_t tile, uint32_t tile_len, Work&& work)
+{
+    if constexpr (!ROWS) {
+        work(g, tile, tile_len);
+    } else {
+        GradTensor p = g;
+        uint32_t rows = 1u;
+        if (g.walk == kGradLong) {
+            const GradRowTiles t(g.row, tile_len);
+            const uint32_t q = tile / t.per_row;
+            const uint64_t r = (uint64_t)q * t.rows;
+            tile -= q * t.per_row;
+            tile_len = t.per_row > 1u ? t.len : tile_len;
+            rows = (uint32_t)min((uint64_t)t.rows, g.n / g.row - r);
+            p.src += r * g.src_stride * (g.src_type == kGradF32 ? 4u : 2u);
+            if (g.dst) p.dst += r * g.dst_stride * (g.dst_type == kGradF32 ? 4u : 2u);
+            p.n = g.row;
+        }
+#pragma unroll 1
+        for (;;) {
+            work(p, tile, tile_len);
+            if (--rows == 0u) break;
+            p.src += (uint64_t)g.src_stride * (g.src_type == kGradF32 ? 4u : 2u);
+            if (g.dst) p.dst += (uint64_t)g.dst_stride * (g.dst_type == kGradF32 ? 4u : 2u);
+        }
+    }
+}
+
+// A tile's place in its tensor, whose elements are counted from `phase` elements before the first one.
 struct TileSpan {
-    uint64_t start;              // of the tile, in elements from the aligned origin
+    uint64_t start;              // of the tile
     uint32_t lo, hi;             // the tensor's elements in the tile: [lo, hi) from the tile's start
 };
 
-__device__ __forceinline__ TileSpan tile_span(const GradEntry& e, uint32_t index, uint32_t tile_log2)
+__device__ __forceinline__ TileSpan tile_span(uint64_t n, uint32_t phase, uint32_t index, uint32_t tile_len)
 {
-    const uint32_t phase = (e.form >> 8) & 15u;
     TileSpan s;
-    s.start = (uint64_t)index << tile_log2;
+    s.start = (uint64_t)index * tile_len;
     s.lo = s.start < phase ? phase - (uint32_t)s.start : 0u;
-    const uint64_t left = e.n + phase - s.start;
-    s.hi = left < (1ull << tile_log2) ? (uint32_t)left : 1u << tile_log2;
+    const uint64_t end = n + phase;                 // (a row's last tile may lie behind it)
+    const uint64_t left = end > s.start ? end - s.start : 0u;
+    s.hi = left < tile_len ? (uint32_t)left : tile_len;
     return s;
 }
 
-// Element offsets of a row-wise tensor: the tile's first element is (row r0, column c0).
-struct RowPlace {
-    uint64_t r0;
-    uint32_t c0;
+// A walk over a tensor of rows in equal steps.
+struct RowCursor {
+    uint64_t at;                 // the element's offset in memory
+    uint64_t step_at;            // what a step adds
+    uint32_t c, step_c, row;     // its column
+    uint32_t gap;                // from the end of one row to the next
+
+    // From element `v` on (of all, in row order), `step` elements at a time.
+    __device__ __forceinline__ RowCursor(uint64_t v, uint32_t step, uint32_t row_, uint32_t stride) : row(row_)
+    {
+        const uint64_t r = v / row;
+        c = (uint32_t)(v - r * row);
+        at = r * stride + c;
+        const uint32_t rows = step / row;
+        step_c = step - rows * row;
+        step_at = (uint64_t)rows * stride + step_c;
+        gap = stride - row;
+    }
+    __device__ __forceinline__ void next()
+    {
+        at += step_at;
+        c += step_c;
+        if (c >= row) {
+            c -= row;
+            at += gap;
+        }
+    }
 };
 
-__device__ __forceinline__ RowPlace row_place(const GradEntry& e, const TileSpan& s)
+// ------------------------------------------------------------------------------------------ values
+// How long L2 keeps what an access touches.
+__device__ __forceinline__ uint64_t l2_policy(bool evict_first)
 {
-    RowPlace p;
-    p.r0 = s.start / e.row;
-    p.c0 = (uint32_t)(s.start - p.r0 * e.row);
-    return p;
+    uint64_t first, normal;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
+    asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
+    return evict_first ? first : normal;
 }
 
-__device__ __forceinline__ void row_offset(const RowPlace& p, uint32_t rel, uint32_t row, uint64_t& r, uint32_t& c)
+__device__ __forceinline__ uint4 load16(const void* p, uint64_t policy)
 {
-    const uint32_t v = p.c0 + rel, q = v / row;          // (c0 < row < 2^31, rel < 2^31)
-    r = p.r0 + q;
-    c = v - q * row;
+    uint4 v;
+    asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p), "l"(policy) : "memory");
+    return v;
 }
 
-// The values of a lane's kGradBatch groups at `rel` (from the tile's start) + 256 j + 8 lane; loose tensors: at rel + 256 j
-// + 32 i + lane.  Elements outside the tensor are 0, and so are the groups that only lie partly inside, or so near an
-// end that an aligned piece of a shifted source would reach past it: those are left to the caller, element by element.
-struct Batch {
-    float x[kGradBatch][8];
-    uint32_t whole;              // bit j: group j was loaded
-};
-
-__device__ __forceinline__ void load_batch(const GradEntry& e, const TileSpan& s, const RowPlace& place, uint32_t rel, Batch& b)
+// 0 where `in` is false.  (One predicated instruction: with a branch around each, loads would not be in flight together.)
+__device__ __forceinline__ uint4 load16_if(bool in, const void* p, uint64_t policy)
 {
-    const uint32_t lane = threadIdx.x & 31u;
-    const uint32_t type = e.form & 3u, walk = (e.form >> 4) & 3u, shift = (e.form >> 12) & 15u;
-    b.whole = 0u;
-    if (walk == kGradLoose) {
-#pragma unroll
-        for (uint32_t j = 0; j < kGradBatch; ++j) {
-#pragma unroll
-            for (uint32_t i = 0; i < 8u; ++i) {
-                const uint32_t v = rel + 256u * j + 32u * i + lane;
-                b.x[j][i] = 0.0f;
-                if (v >= s.lo && v < s.hi) {
-                    uint64_t r;
-                    uint32_t c;
-                    row_offset(place, v, e.row, r, c);
-                    b.x[j][i] = load_element(e.src, r * e.src_stride + c, type);
-                }
-            }
-        }
-        return;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("{\n\t.reg .pred in;\n\tsetp.ne.u32 in, %6, 0;\n\t"
+                 "@in ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;\n\t}"
+                 : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w) : "l"(p), "l"(policy), "r"((uint32_t)in) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ uint2 load8(const void* p, uint64_t policy)
+{
+    uint2 v;
+    asm volatile("ld.global.L2::cache_hint.v2.u32 {%0, %1}, [%2], %3;" : "=r"(v.x), "=r"(v.y) : "l"(p), "l"(policy) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void store16(void* p, uint4 v, uint64_t policy)
+{
+    asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w),
+                 "l"(policy) : "memory");
+}
+
+__device__ __forceinline__ void store8(void* p, uint2 v, uint64_t policy)
+{
+    asm volatile("st.global.L2::cache_hint.v2.u32 [%0], {%1, %2}, %3;" ::"l"(p), "r"(v.x), "r"(v.y), "l"(policy) : "memory");
+}
+
+__device__ __forceinline__ float load_element(const char* p, uint64_t i, uint32_t type)
+{
+    if (type == kGradF32) return reinterpret_cast<const float*>(p)[i];
+    const uint16_t h = reinterpret_cast<const uint16_t*>(p)[i];
+    return type == kGradBF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
+}
+
+// One rounding, of the product in fp32 to the destination's type (to nearest, ties to even).
+__device__ __forceinline__ void store_element(char* p, uint64_t i, uint32_t type, float x)
+{
+    if (type == kGradF32)
+        reinterpret_cast<float*>(p)[i] = x;
+    else if (type == kGradBF16)
+        reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
+    else
+        reinterpret_cast<__half*>(p)[i] = __float2half_rn(x);
+}
+
+// The two values of a word.
+__device__ __forceinline__ float2 widen(uint32_t w, uint32_t type)
+{
+    if (type == kGradBF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+__device__ __forceinline__ uint32_t narrow(float a, float b, uint32_t type)
+{
+    if (type == kGradBF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
     }
-    // byte address of the group's first element, and of the aligned piece that holds it
-    const uint32_t size = type == kGradF32 ? 4u : 2u;
-    const char* p[kGradBatch];
-    const uint32_t margin = shift ? 8u : 0u;
-#pragma unroll
-    for (uint32_t j = 0; j < kGradBatch; ++j) {
-        const uint32_t v = rel + 256u * j + 8u * lane;
-        if (v >= s.lo && v + 8u <= s.hi) {
-            // (the margin is counted from the ends of the tensor, not of the tile)
-            const uint64_t at = s.start + v, phase = (e.form >> 8) & 15u;
-            if (!margin || (at >= phase + margin && at + 8u + margin <= phase + e.n)) b.whole |= 1u << j;
-        }
-        if (walk == kGradRows) {
-            uint64_t r;
-            uint32_t c;
-            row_offset(place, v, e.row, r, c);
-            p[j] = static_cast<const char*>(e.src) + (r * e.src_stride + c) * size;
-        } else {
-            p[j] = static_cast<const char*>(e.src) - (uint64_t)((e.form >> 8) & 15u) * size - shift + (s.start + v) * size;
-        }
-    }
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    if (type == kGradF32) {
-        if (shift == 0u) {
-            uint4 q[kGradBatch][2];
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                const uint4* a = reinterpret_cast<const uint4*>(p[j]);
-                const bool in = b.whole >> j & 1u;
-                q[j][0] = in ? a[0] : zero;
-                q[j][1] = in ? a[1] : zero;
-            }
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    b.x[j][4 * h] = __uint_as_float(q[j][h].x);
-                    b.x[j][4 * h + 1] = __uint_as_float(q[j][h].y);
-                    b.x[j][4 * h + 2] = __uint_as_float(q[j][h].z);
-                    b.x[j][4 * h + 3] = __uint_as_float(q[j][h].w);
-                }
-            }
-        } else {
-            uint4 q[kGradBatch][3];
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                const uint4* a = reinterpret_cast<const uint4*>(p[j]);
-                const bool in = b.whole >> j & 1u;
-                q[j][0] = in ? a[0] : zero;
-                q[j][1] = in ? a[1] : zero;
-                q[j][2] = in ? a[2] : zero;
-            }
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                uint32_t w[8];
-                shifted_words<3, 8, false>(q[j], shift, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) b.x[j][i] = __uint_as_float(w[i]);
-            }
-        }
-    } else {
-        uint32_t w[kGradBatch][4];
-        if (shift == 0u) {
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                const uint4 q = (b.whole >> j & 1u) ? *reinterpret_cast<const uint4*>(p[j]) : zero;
-                w[j][0] = q.x;
-                w[j][1] = q.y;
-                w[j][2] = q.z;
-                w[j][3] = q.w;
-            }
-        } else {
-            uint4 q[kGradBatch][2];
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                const uint4* a = reinterpret_cast<const uint4*>(p[j]);
-                const bool in = b.whole >> j & 1u;
-                q[j][0] = in ? a[0] : zero;
-                q[j][1] = in ? a[1] : zero;
-            }
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) shifted_words<2, 4, true>(q[j], shift, w[j]);
-        }
-        if (type == kGradBF16) {
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) widen_bf16(w[j], b.x[j]);
-        } else {
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) widen_f16(w[j], b.x[j]);
-        }
-    }
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 // ------------------------------------------------------------------------------------------ norm
@@ -318,8 +333,8 @@ template <> struct NormPart<false> {
     double s;
     __device__ __forceinline__ void add(float x)
     {
-        const double d = (double)x;
-        s = __fma_rn(d, d, s);
+        // (volatile: in this order, or dozens of values in 64 bits would be alive at once)
+        asm volatile("{\n\t.reg .f64 d;\n\tcvt.f64.f32 d, %1;\n\tfma.rn.f64 %0, d, d, %0;\n\t}" : "+d"(s) : "f"(x));
     }
     __device__ __forceinline__ void join(const NormPart& o) { s = __dadd_rn(s, o.s); }
     __device__ __forceinline__ NormPart other(int lane_mask) const
@@ -333,11 +348,7 @@ template <> struct NormPart<false> {
 
 template <> struct NormPart<true> {
     uint64_t s;
-    __device__ __forceinline__ void add(float x)
-    {
-        const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
-        s = max((uint32_t)s, u);
-    }
+    __device__ __forceinline__ void add(float x) { s = max((uint32_t)s, __float_as_uint(x) & 0x7FFFFFFFu); }
     __device__ __forceinline__ void join(const NormPart& o) { s = max((uint32_t)s, (uint32_t)o.s); }
     __device__ __forceinline__ NormPart other(int lane_mask) const
     {
@@ -370,32 +381,105 @@ __device__ __forceinline__ void reduce_block(NormPart<MAX>& a, NormPart<MAX>* pa
     }
 }
 
-// Adds one tile of a tensor to a lane's part.
-template <bool MAX>
-__device__ __forceinline__ void norm_tile(const GradEntry& e, uint32_t index, uint32_t tile_log2, NormPart<MAX>& acc)
+// Adds the 16-byte pieces of a lane.  Halves of the maximum of 16-bit types are kept in `pair`, one pattern in each.
+template <bool MAX, bool F32, int P>
+__device__ __forceinline__ void norm_pieces(const uint4 (&q)[P], uint32_t type, NormPart<MAX> (&acc)[2], uint32_t& pair)
 {
-    const TileSpan s = tile_span(e, index, tile_log2);
-    const uint32_t walk = (e.form >> 4) & 3u;
-    RowPlace place = {0u, 0u};
-    if (walk != kGradFlat) place = row_place(e, s);
-    for (uint32_t rel = 0u; rel < s.hi; rel += 1u << kGradTileLog2) {
-        Batch b;
-        load_batch(e, s, place, rel, b);
 #pragma unroll
-        for (uint32_t j = 0; j < kGradBatch; ++j) {
+    for (int j = 0; j < P; ++j) {
+        const uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc.add(b.x[j][i]);
-        }
-        if (walk == kGradLoose) continue;
-        const uint32_t type = e.form & 3u, phase = (e.form >> 8) & 15u;
-#pragma unroll 1
-        for (uint32_t j = 0; j < kGradBatch; ++j) {
-            const uint32_t v = rel + 256u * j + 8u * (threadIdx.x & 31u);
-            if ((b.whole >> j & 1u) || v + 8u <= s.lo || v >= s.hi) continue;
-#pragma unroll 1
-            for (uint32_t i = max(v, s.lo); i < min(v + 8u, s.hi); ++i) acc.add(load_element(e.src, s.start + i - phase, type));
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (F32) {
+                acc[i & 1].add(__uint_as_float(w[i]));
+            } else if constexpr (MAX) {
+                pair = __vmaxu2(pair, w[i] & 0x7FFF7FFFu);
+            } else {
+                const float2 x = widen(w[i], type);
+                acc[0].add(x.x);
+                acc[1].add(x.y);
+            }
         }
     }
+}
+
+// The pieces of a lane among `count` of a tile; address() gives one after the other.
+template <bool MAX, bool F32, class Address>
+__device__ __forceinline__ void norm_piece_range(uint32_t count, uint32_t type, uint64_t policy, NormPart<MAX> (&acc)[2],
+                                                 uint32_t& pair, Address&& address)
+{
+    constexpr uint32_t kFlight = 8;
+    for (uint32_t p = threadIdx.x & 31u; p < count; p += 32u * kFlight) {
+        uint4 q[kFlight];
+#pragma unroll
+        for (uint32_t j = 0; j < kFlight; ++j) {
+            const uint4* a = address();
+            q[j] = load16_if(p + 32u * j < count, a, policy);
+        }
+        norm_pieces<MAX, F32>(q, type, acc, pair);
+    }
+}
+
+template <bool ROWS, bool MAX, bool F32>
+__device__ __forceinline__ void norm_tile(const GradTensor& g, uint32_t index, uint32_t tile_len, uint64_t policy,
+                                          NormPart<MAX> (&acc)[2])
+{
+    constexpr uint32_t kSize = F32 ? 4u : 2u, kPerPiece = 16u / kSize;
+    const uint32_t lane = threadIdx.x & 31u;
+    uint32_t pair = 0u;
+    if (!ROWS || g.walk <= kGradLong) {
+        // the tile's elements, which begin at an aligned address only where the source sets the phase
+        const uint32_t phase = tile_phase(g);
+        const TileSpan s = tile_span(g.n, phase, index, tile_len);
+        const char* first = g.src + (s.start + s.lo - phase) * kSize;
+        const uint32_t count = s.hi - s.lo;
+        const uint32_t head = min(count, (uint32_t)(0u - reinterpret_cast<uintptr_t>(first) / kSize) % kPerPiece);
+        const uint32_t whole = (count - head) / kPerPiece;
+        const uint4* pieces = reinterpret_cast<const uint4*>(first + head * kSize) + lane;
+        norm_piece_range<MAX, F32>(whole, g.src_type, policy, acc, pair, [&] {
+            const uint4* a = pieces;
+            pieces += 32;
+            return a;
+        });
+        const uint32_t behind = head + whole * kPerPiece + lane;
+        if (lane < head) acc[0].add(load_element(first, lane, g.src_type));
+        if (behind < count) acc[1].add(load_element(first, behind, g.src_type));
+    } else if constexpr (ROWS) {
+        const TileSpan s = tile_span(g.n, 0u, index, tile_len);
+        if (g.walk == kGradWide) {
+            RowCursor cur(s.start + lane * kPerPiece, 32u * kPerPiece, g.row, g.src_stride);
+            norm_piece_range<MAX, F32>(s.hi / kPerPiece, g.src_type, policy, acc, pair, [&] {
+                const uint4* a = reinterpret_cast<const uint4*>(g.src + cur.at * kSize);
+                cur.next();
+                return a;
+            });
+        } else {
+            RowCursor cur(s.start + lane, 32u, g.row, g.src_stride);
+#pragma unroll 4
+            for (uint32_t v = lane; v < s.hi; v += 32u) {
+                acc[0].add(load_element(g.src, cur.at, g.src_type));
+                cur.next();
+            }
+        }
+    }
+    if constexpr (MAX && !F32) {
+        const float2 x = widen(pair, g.src_type);
+        acc[0].add(x.x);
+        acc[1].add(x.y);
+    }
+}
+
+// Adds one tile of a tensor to a lane's part.
+template <bool ROWS, bool MAX>
+__device__ __forceinline__ void norm_tile(const GradTensor& g, uint32_t tile, uint32_t tile_len, uint64_t policy,
+                                          NormPart<MAX> (&acc)[2])
+{
+    for_pieces<ROWS>(g, tile, tile_len, [&](const GradTensor& p, uint32_t index, uint32_t len) {
+        if (p.src_type == kGradF32)
+            norm_tile<ROWS, MAX, true>(p, index, len, policy, acc);
+        else
+            norm_tile<ROWS, MAX, false>(p, index, len, policy, acc);
+    });
 }
 
 // Writes the norm and reports one that is no finite number.
@@ -406,65 +490,63 @@ __device__ __forceinline__ void publish_norm(float norm, float* out_norm, uint32
 }
 
 // A part of the norm per CTA (slots[blockIdx]), or with EACH per tile (slots[tile]).
-template <class Table, bool MAX, bool EACH>
-__global__ void __launch_bounds__(kGradThreads)
+template <class Table, bool ROWS, bool MAX, bool EACH>
+__global__ void __launch_bounds__(kGradThreads, kGradNormCtas)
 grad_norm_kernel(const __grid_constant__ Table t, NormPart<MAX>* slots)
 {
     __shared__ NormPart<MAX> parts[kGradWarps];
+    const uint32_t tiles = t.first_tile[t.count], first = blockIdx.x * kGradWarps + (threadIdx.x >> 5);
+    NormPart<MAX> acc[2] = {};
+    TensorRun run;
+    run.start<ROWS>(t, first, tiles);
     grid_dependency_wait();
     grid_dependency_launch_next();
-    const uint32_t tiles = t.first_tile[t.count];
-    const uint32_t begin = (uint32_t)((uint64_t)tiles * blockIdx.x / gridDim.x);
-    const uint32_t end = (uint32_t)((uint64_t)tiles * (blockIdx.x + 1u) / gridDim.x);
-    NormPart<MAX> acc = {};
-    for (uint32_t tile = begin + (threadIdx.x >> 5); tile < end; tile += kGradWarps) {
-        const uint32_t k = find_tensor(t, tile);
-        norm_tile<MAX>(t.e[k], tile - t.first_tile[k], t.tile_log2, acc);
+    for (uint32_t tile = first; tile < tiles; tile += gridDim.x * kGradWarps) {
+        if (tile >= run.end) run.seek<ROWS>(t, tile);
+        norm_tile<ROWS, MAX>(run.g, tile - run.first, t.tile_len, l2_policy(tile < t.stream_below), acc);
         if constexpr (EACH) {
-            reduce_warp(acc);
-            if ((threadIdx.x & 31u) == 0u) slots[tile] = acc;
-            acc = {};
+            acc[0].join(acc[1]);
+            reduce_warp(acc[0]);
+            if ((threadIdx.x & 31u) == 0u) slots[tile] = acc[0];
+            acc[0] = acc[1] = {};
         }
     }
     if constexpr (!EACH) {
-        reduce_block(acc, parts, kGradWarps);
-        if (threadIdx.x == 0u) slots[blockIdx.x] = acc;
+        acc[0].join(acc[1]);
+        reduce_block(acc[0], parts, kGradWarps);
+        if (threadIdx.x == 0u) slots[blockIdx.x] = acc[0];
     }
 }
 
-// The whole from the slots of all launches before it.
+// The whole from the slots of all launches before it (CTA 0, where `out_norm` is given), and the norms of single tensors
+// from the slots of their tiles, a warp each: tensor i of the launch owns the slots [first[i], first[i + 1]).
 constexpr int kGradJoinThreads = 1024;
 
-template <bool MAX>
+template <int N>
+struct GradEachTable {
+    static constexpr int kCapacity = N;
+    uint32_t count;
+    uint32_t first[N + 1];
+};
+
+template <class Table, bool MAX>
 __global__ void __launch_bounds__(kGradJoinThreads)
-grad_norm_join_kernel(const NormPart<MAX>* slots, uint32_t num_slots, float* out_norm, uint32_t* status)
+grad_norm_join_kernel(const __grid_constant__ Table t, const NormPart<MAX>* slots, uint32_t num_slots, float* out_norm,
+                      float* out_norms, uint32_t* status)
 {
     __shared__ NormPart<MAX> parts[kGradJoinThreads / 32];
     grid_dependency_wait();
     grid_dependency_launch_next();
     NormPart<MAX> acc = {};
-    for (uint32_t i = threadIdx.x; i < num_slots; i += kGradJoinThreads) acc.join(slots[i]);
-    reduce_block(acc, parts, kGradJoinThreads / 32);
-    if (threadIdx.x == 0u) publish_norm(acc.norm(), out_norm, status);
-}
-
-// The norms of single tensors from the slots of their tiles; tensor i of the launch owns the slots [first[i], first[i + 1]).
-constexpr int kGradEachCapacity = 8000;
-
-struct GradEachTable {
-    uint32_t count;
-    uint32_t first[kGradEachCapacity + 1];
-};
-
-template <bool MAX>
-__global__ void __launch_bounds__(kGradThreads)
-grad_norms_each_kernel(const __grid_constant__ GradEachTable t, const NormPart<MAX>* slots, float* out_norms)
-{
-    grid_dependency_wait();
-    grid_dependency_launch_next();
-    const uint32_t i = blockIdx.x * kGradWarps + (threadIdx.x >> 5);
+    if (blockIdx.x == 0u) {
+        if (!out_norm) return;
+        for (uint32_t i = threadIdx.x; i < num_slots; i += kGradJoinThreads) acc.join(slots[i]);
+        reduce_block(acc, parts, kGradJoinThreads / 32);
+        if (threadIdx.x == 0u) publish_norm(acc.norm(), out_norm, status);
+        return;
+    }
+    const uint32_t i = (blockIdx.x - 1u) * (kGradJoinThreads / 32u) + (threadIdx.x >> 5);
     if (i >= t.count) return;
-    NormPart<MAX> acc = {};
     for (uint32_t k = t.first[i] + (threadIdx.x & 31u); k < t.first[i + 1u]; k += 32u) acc.join(slots[k]);
     reduce_warp(acc);
     if ((threadIdx.x & 31u) == 0u) out_norms[i] = acc.norm();
@@ -479,7 +561,9 @@ struct ClipArgs {
     const float* norm;
     float* out_norm;             // optional
     uint32_t* status;            // optional
-    uint32_t in_place;
+    uint16_t in_place;           // the destination is the source
+    uint8_t max_kind;            // the slots are maxima
+    uint8_t stream;              // the destination is not wanted in L2 for long
 };
 
 __device__ __forceinline__ float clip_factor(float norm, float max_norm)
@@ -487,109 +571,269 @@ __device__ __forceinline__ float clip_factor(float norm, float max_norm)
     return norm <= max_norm ? 1.0f : __fdiv_rn(max_norm, norm);
 }
 
-// Multiplies one tile by c into the destination.
-__device__ __forceinline__ void scale_tile(const GradEntry& e, uint32_t index, uint32_t tile_log2, float c)
-{
-    const TileSpan s = tile_span(e, index, tile_log2);
-    const uint32_t walk = (e.form >> 4) & 3u, type = (e.form >> 2) & 3u;
-    const uint32_t lane = threadIdx.x & 31u;
-    RowPlace place = {0u, 0u};
-    if (walk != kGradFlat) place = row_place(e, s);
-    for (uint32_t rel = 0u; rel < s.hi; rel += 1u << kGradTileLog2) {
-        Batch b;
-        load_batch(e, s, place, rel, b);
-#pragma unroll
-        for (uint32_t j = 0; j < kGradBatch; ++j) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b.x[j][i] = __fmul_rn(b.x[j][i], c);
-        }
-        if (walk == kGradLoose) {
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-#pragma unroll
-                for (uint32_t i = 0; i < 8u; ++i) {
-                    const uint32_t v = rel + 256u * j + 32u * i + lane;
-                    if (v >= s.lo && v < s.hi) {
-                        uint64_t r;
-                        uint32_t col;
-                        row_offset(place, v, e.row, r, col);
-                        store_element(e.dst, r * e.dst_stride + col, type, b.x[j][i]);
-                    }
-                }
-            }
-            continue;
-        }
-        const uint32_t size = type == kGradF32 ? 4u : 2u, phase = (e.form >> 8) & 15u;
-        char* p[kGradBatch];
-#pragma unroll
-        for (uint32_t j = 0; j < kGradBatch; ++j) {
-            const uint32_t v = rel + 256u * j + 8u * lane;
-            uint64_t at = s.start + v - phase;
-            if (walk == kGradRows) {
-                uint64_t r;
-                uint32_t col;
-                row_offset(place, v, e.row, r, col);
-                at = r * e.dst_stride + col;
-            }
-            p[j] = static_cast<char*>(e.dst) + at * size;
-        }
-        if (type == kGradF32) {
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                if (b.whole >> j & 1u) {
-                    float4* a = reinterpret_cast<float4*>(p[j]);
-                    a[0] = make_float4(b.x[j][0], b.x[j][1], b.x[j][2], b.x[j][3]);
-                    a[1] = make_float4(b.x[j][4], b.x[j][5], b.x[j][6], b.x[j][7]);
-                }
-            }
+// A lane's unit of work: the elements that are 16 bytes on the wider side, so that a warp's loads and stores are contiguous.
+template <bool SF32, bool DF32> constexpr uint32_t kGradGroup = SF32 || DF32 ? 4u : 8u;
+
+// 16 or 8 bytes as words.
+template <int W> struct GradPiece {
+    uint32_t w[W];
+    __device__ __forceinline__ void load(const char* p, uint64_t policy)
+    {
+        if constexpr (W == 4) {
+            const uint4 v = load16(p, policy);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
         } else {
-#pragma unroll
-            for (uint32_t j = 0; j < kGradBatch; ++j) {
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (type == kGradBF16) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(b.x[j][2 * i], b.x[j][2 * i + 1]);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                    } else {
-                        const __half2 h = __floats2half2_rn(b.x[j][2 * i], b.x[j][2 * i + 1]);
-                        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                }
-                if (b.whole >> j & 1u) *reinterpret_cast<uint4*>(p[j]) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            const uint2 v = load8(p, policy);
+            w[0] = v.x, w[1] = v.y;
         }
+    }
+};
+
+// The words that start `shift` bytes (whole elements) into a, with what lies behind it: the next lane's piece, and behind
+// the last lane's the first lane's next one.  The piece's own size is the most that it can be shifted by.
+template <int W, bool HALF>
+__device__ __forceinline__ GradPiece<W> shifted(const GradPiece<W>& a, const GradPiece<W>& next, uint32_t shift)
+{
+    constexpr int kBehind = HALF ? W : W - 1;              // words that are needed from behind
+    const uint32_t lane = threadIdx.x & 31u;
+    uint32_t v[2 * W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        v[i] = a.w[i];
+        if (i < kBehind) v[W + i] = __shfl_sync(0xFFFFFFFFu, lane == 0u ? next.w[i] : a.w[i], lane + 1u);
+        else v[W + i] = 0u;
+    }
+    if constexpr (W == 4) {
+        if (shift & 8u) {
+#pragma unroll
+            for (int i = 0; i + 2 < 2 * W; ++i) v[i] = v[i + 2];
+        }
+    }
+    if (shift & 4u) {
+#pragma unroll
+        for (int i = 0; i + 1 < 2 * W; ++i) v[i] = v[i + 1];
+    }
+    GradPiece<W> out;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        out.w[i] = v[i];
+        if constexpr (HALF) {
+            if (shift & 2u) out.w[i] = __funnelshift_r(v[i], v[i + 1], 16);
+        }
+    }
+    return out;
+}
+
+// The factor, and the L2 policies of both sides.
+struct Scaling {
+    float c;
+    uint64_t src, dst;
+};
+
+// A group, from the words it was read as to its destination.
+template <bool SF32, bool DF32, int W>
+__device__ __forceinline__ void store_group(const GradPiece<W>& w, const GradTensor& g, const Scaling& f, char* d)
+{
+    constexpr uint32_t kGroup = kGradGroup<SF32, DF32>;
+    float x[kGroup];
+#pragma unroll
+    for (uint32_t i = 0; i < kGroup; i += 2u) {
+        float2 v;
+        if constexpr (SF32)
+            v = make_float2(__uint_as_float(w.w[i]), __uint_as_float(w.w[i + 1u]));
+        else
+            v = widen(w.w[i / 2u], g.src_type);
+        x[i] = __fmul_rn(v.x, f.c);
+        x[i + 1u] = __fmul_rn(v.y, f.c);
+    }
+    if constexpr (DF32) {
+        store16(d, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])), f.dst);
+    } else if constexpr (kGroup == 4u) {
+        store8(d, make_uint2(narrow(x[0], x[1], g.dst_type), narrow(x[2], x[3], g.dst_type)), f.dst);
+    } else {
+        store16(d, make_uint4(narrow(x[0], x[1], g.dst_type), narrow(x[2], x[3], g.dst_type), narrow(x[4], x[5], g.dst_type),
+                              narrow(x[6], x[7], g.dst_type)), f.dst);
+    }
+}
+
+// The next kFlight groups of every lane of a contiguous tile; with EDGE those from `left` on are no longer the tile's: the
+// last one that may be read is read again, and nothing is stored.
+template <bool SF32, bool DF32, bool SHIFT, bool EDGE, uint32_t kFlight>
+__device__ __forceinline__ void scale_batch(const char* src, char* dst, uint32_t left, const GradTensor& g, uint32_t shift,
+                                            const Scaling& f)
+{
+    constexpr uint32_t kGroup = kGradGroup<SF32, DF32>;
+    constexpr uint32_t kSrc = kGroup * (SF32 ? 4u : 2u), kDst = kGroup * (DF32 ? 4u : 2u);
+    const uint32_t lane = threadIdx.x & 31u, last = SHIFT ? left : left - 1u;
+    auto from = [&](uint32_t p) { return src + (EDGE ? min(p, last) : p) * kSrc; };
+    GradPiece<kSrc / 4u> q[kFlight + (SHIFT ? 1 : 0)];
+#pragma unroll
+    for (uint32_t j = 0; j < kFlight; ++j) q[j].load(from(32u * j + lane), f.src);
+    if constexpr (SHIFT) q[kFlight].load(from(32u * kFlight), f.src);
+#pragma unroll
+    for (uint32_t j = 0; j < kFlight; ++j) {
+        GradPiece<kSrc / 4u> w = q[j];
+        if constexpr (SHIFT) w = shifted<kSrc / 4u, !SF32>(q[j], q[j + 1u], shift);
+        const uint32_t p = 32u * j + lane;
+        if (!EDGE || p < left) store_group<SF32, DF32>(w, g, f, dst + p * kDst);
+    }
+}
+
+// The whole groups [begin, end) of a contiguous tile, eight of a lane in flight (four of 16-bit elements on both sides).
+// Group p lies at src + p and dst + p groups, both aligned to the group's size there; the source there is `shift` bytes
+// before the group's first element, and group `end` may be read too where shift is not 0.
+template <bool SF32, bool DF32, bool SHIFT>
+__device__ __forceinline__ void scale_groups(uint32_t begin, uint32_t end, const GradTensor& g, uint32_t shift, const Scaling& f,
+                                             const char* src, char* dst)
+{
+    constexpr uint32_t kGroup = kGradGroup<SF32, DF32>, kFlight = kGroup == 8u ? 4u : 8u;
+    constexpr uint32_t kSrc = kGroup * (SF32 ? 4u : 2u), kDst = kGroup * (DF32 ? 4u : 2u);
+    uint32_t left = end - begin;
+    src += begin * kSrc;
+    dst += begin * kDst;
+    for (; left >= 32u * kFlight; left -= 32u * kFlight) {
+        scale_batch<SF32, DF32, SHIFT, false, kFlight>(src, dst, left, g, shift, f);
+        src += 32u * kFlight * kSrc;
+        dst += 32u * kFlight * kDst;
+    }
 #pragma unroll 1
-        for (uint32_t j = 0; j < kGradBatch; ++j) {
-            const uint32_t v = rel + 256u * j + 8u * lane;
-            if ((b.whole >> j & 1u) || v + 8u <= s.lo || v >= s.hi) continue;
-#pragma unroll 1
-            for (uint32_t i = max(v, s.lo); i < min(v + 8u, s.hi); ++i) {
-                const uint64_t at = s.start + i - phase;
-                store_element(e.dst, at, type, __fmul_rn(load_element(e.src, at, e.form & 3u), c));
+    while (left != 0u) {
+        scale_batch<SF32, DF32, SHIFT, true, 4u>(src, dst, left, g, shift, f);
+        left -= min(left, 128u);
+        src += 128u * kSrc;
+        dst += 128u * kDst;
+    }
+}
+
+// The groups of a tile of a tensor in rows.
+template <bool SF32, bool DF32>
+__device__ __forceinline__ void scale_row_groups(const TileSpan& s, const GradTensor& g, const Scaling& f)
+{
+    constexpr uint32_t kGroup = kGradGroup<SF32, DF32>, kFlight = 4u;
+    constexpr uint32_t kSrc = kGroup * (SF32 ? 4u : 2u), kDst = kGroup * (DF32 ? 4u : 2u);
+    const uint32_t end = s.hi / kGroup;
+    const uint64_t v = s.start + (threadIdx.x & 31u) * kGroup;
+    RowCursor from(v, 32u * kGroup, g.row, g.src_stride), to(v, 32u * kGroup, g.row, g.dst_stride);
+    for (uint32_t p = threadIdx.x & 31u; p < end; p += 32u * kFlight) {
+        GradPiece<kSrc / 4u> q[kFlight] = {};
+#pragma unroll
+        for (uint32_t j = 0; j < kFlight; ++j) {
+            if (p + 32u * j < end) q[j].load(g.src + from.at * (kSrc / kGroup), f.src);
+            from.next();
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kFlight; ++j) {
+            if (p + 32u * j < end) store_group<SF32, DF32>(q[j], g, f, g.dst + to.at * (kDst / kGroup));
+            to.next();
+        }
+    }
+}
+
+template <bool ROWS, bool SF32, bool DF32>
+__device__ __forceinline__ void scale_tile(const GradTensor& g, uint32_t index, uint32_t tile_len, const Scaling& f)
+{
+    constexpr uint32_t kSrc = SF32 ? 4u : 2u, kDst = DF32 ? 4u : 2u, kGroup = kGradGroup<SF32, DF32>;
+    const uint32_t lane = threadIdx.x & 31u;
+    if (!ROWS || g.walk <= kGradLong) {
+        const uint32_t phase = tile_phase(g);
+        const TileSpan s = tile_span(g.n, phase, index, tile_len);
+        const char* src = g.src - phase * kSrc;
+        char* dst = g.dst - phase * kDst;
+        const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(src) & (kGroup * kSrc - 1u);
+        uint32_t lo = s.lo, hi = s.hi;
+        if (shift) {
+            // the pieces of a shifted group reach up to a group before and behind it: not past the tensor
+            if (s.start < phase + kGroup) lo = phase + kGroup - (uint32_t)s.start;
+            const uint64_t left = g.n + phase - s.start;
+            if (left < (uint64_t)hi + kGroup) hi = left < kGroup ? 0u : (uint32_t)left - kGroup;
+        }
+        const uint32_t begin = (lo + kGroup - 1u) / kGroup, end = max(begin, hi / kGroup);
+        const char* a = src + s.start * kSrc - shift;
+        char* b = dst + s.start * kDst;
+        if (shift)
+            scale_groups<SF32, DF32, true>(begin, end, g, shift, f, a, b);
+        else
+            scale_groups<SF32, DF32, false>(begin, end, g, 0u, f, a, b);
+        // what lies before the first of these groups and behind the last one: at most 15 elements each
+        const uint32_t before = s.lo + lane, behind = end * kGroup + lane;
+        if (before < min(begin * kGroup, s.hi))
+            store_element(dst, s.start + before, g.dst_type, __fmul_rn(load_element(src, s.start + before, g.src_type), f.c));
+        if (behind < s.hi)
+            store_element(dst, s.start + behind, g.dst_type, __fmul_rn(load_element(src, s.start + behind, g.src_type), f.c));
+    } else if constexpr (ROWS) {
+        const TileSpan s = tile_span(g.n, 0u, index, tile_len);
+        if (g.walk == kGradWide) {
+            scale_row_groups<SF32, DF32>(s, g, f);
+        } else {
+            RowCursor from(s.start + lane, 32u, g.row, g.src_stride), to(s.start + lane, 32u, g.row, g.dst_stride);
+#pragma unroll 4
+            for (uint32_t v = lane; v < s.hi; v += 32u) {
+                store_element(g.dst, to.at, g.dst_type, __fmul_rn(load_element(g.src, from.at, g.src_type), f.c));
+                from.next();
+                to.next();
             }
         }
     }
 }
 
+// Multiplies one tile by c into the destination.
+template <bool ROWS>
+__device__ __forceinline__ void scale_tile(const GradTensor& g, uint32_t tile, uint32_t tile_len, const Scaling& f)
+{
+    for_pieces<ROWS>(g, tile, tile_len, [&](const GradTensor& p, uint32_t index, uint32_t len) {
+        if (p.src_type == kGradF32) {
+            if (p.dst_type == kGradF32)
+                scale_tile<ROWS, true, true>(p, index, len, f);
+            else
+                scale_tile<ROWS, true, false>(p, index, len, f);
+        } else {
+            if (p.dst_type == kGradF32)
+                scale_tile<ROWS, false, true>(p, index, len, f);
+            else
+                scale_tile<ROWS, false, false>(p, index, len, f);
+        }
+    });
+}
+
 // The last tiles first: they are what the norm's pass has left in L2.
-template <class Table, bool MAX>
-__global__ void __launch_bounds__(kGradThreads)
+// The norm from its parts, by one warp: every CTA begins with it, so all loads of up to 640 parts are in flight together.
+template <bool MAX>
+__device__ __forceinline__ float joined_norm(const ClipArgs& a)
+{
+    constexpr uint32_t kFlight = 20;
+    const NormPart<MAX>* slots = static_cast<const NormPart<MAX>*>(a.slots);
+    NormPart<MAX> acc = {};
+    for (uint32_t i = threadIdx.x & 31u; i < a.num_slots; i += 32u * kFlight) {
+        NormPart<MAX> part[kFlight];
+#pragma unroll
+        for (uint32_t j = 0; j < kFlight; ++j) {
+            part[j] = slots[min(i + 32u * j, a.num_slots - 1u)];
+            if (i + 32u * j >= a.num_slots) part[j] = {};
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kFlight; ++j) acc.join(part[j]);
+    }
+    reduce_warp(acc);
+    return acc.norm();
+}
+
+template <class Table, bool ROWS>
+__global__ void __launch_bounds__(kGradThreads, kGradScaleCtas)
 grad_scale_kernel(const __grid_constant__ Table t, const __grid_constant__ ClipArgs a)
 {
-    __shared__ NormPart<MAX> parts[kGradWarps];
     __shared__ float factor;
+    const uint32_t tiles = t.first_tile[t.count], first = blockIdx.x * kGradWarps + (threadIdx.x >> 5);
+    TensorRun run;
+    run.start<ROWS>(t, tiles - 1u - first, tiles);
     grid_dependency_wait();
     float c = 1.0f;
     if (a.num_slots) {
-        NormPart<MAX> acc = {};
-        for (uint32_t i = threadIdx.x; i < a.num_slots; i += kGradThreads)
-            acc.join(static_cast<const NormPart<MAX>*>(a.slots)[i]);
-        reduce_block(acc, parts, kGradWarps);
-        if (threadIdx.x == 0u) {
-            const float norm = acc.norm();
-            factor = clip_factor(norm, a.max_norm);
-            if (blockIdx.x == 0u) publish_norm(norm, a.out_norm, a.status);
+        if (threadIdx.x < 32u) {
+            const float norm = a.max_kind ? joined_norm<true>(a) : joined_norm<false>(a);
+            if (threadIdx.x == 0u) {
+                factor = clip_factor(norm, a.max_norm);
+                if (blockIdx.x == 0u) publish_norm(norm, a.out_norm, a.status);
+            }
         }
         __syncthreads();
         c = factor;
@@ -600,19 +844,18 @@ grad_scale_kernel(const __grid_constant__ Table t, const __grid_constant__ ClipA
     }
     grid_dependency_launch_next();
     if (a.in_place && c == 1.0f) return;
-    const uint32_t tiles = t.first_tile[t.count], cta = gridDim.x - 1u - blockIdx.x;
-    const uint32_t begin = (uint32_t)((uint64_t)tiles * cta / gridDim.x);
-    const uint32_t end = (uint32_t)((uint64_t)tiles * (cta + 1u) / gridDim.x);
-    for (uint32_t tile = begin + (threadIdx.x >> 5); tile < end; tile += kGradWarps) {
-        const uint32_t k = find_tensor(t, tile);
-        scale_tile(t.e[k], tile - t.first_tile[k], t.tile_log2, c);
+    const Scaling f = {c, l2_policy(true), l2_policy(a.stream != 0u)};
+    for (uint32_t i = first; i < tiles; i += gridDim.x * kGradWarps) {
+        const uint32_t tile = tiles - 1u - i;
+        if (tile < run.first || tile >= run.end) run.seek<ROWS>(t, tile);
+        scale_tile<ROWS>(run.g, tile - run.first, t.tile_len, f);
     }
 }
 
 // ------------------------------------------------------------------------------------------ short lists
 // Norm and clipping of a short list in one launch: a cluster of CTAs whose parts of the norm meet over distributed
 // shared memory.  SCALE: multiplies as well.  Two launches that wait for one another cost more than the work.
-template <class Table, bool MAX, bool SCALE>
+template <class Table, bool ROWS, bool MAX, bool SCALE>
 __global__ void __launch_bounds__(kGradClusterThreads)
 grad_cluster_kernel(const __grid_constant__ Table t, const __grid_constant__ ClipArgs a)
 {
@@ -620,17 +863,20 @@ grad_cluster_kernel(const __grid_constant__ Table t, const __grid_constant__ Cli
     __shared__ NormPart<MAX> parts[kWarps];
     __shared__ NormPart<MAX> mine;
     __shared__ float factor;
-    grid_dependency_wait();
-    grid_dependency_launch_next();
     const uint32_t tiles = t.first_tile[t.count], step = gridDim.x * kWarps;
     const uint32_t first = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
-    NormPart<MAX> acc = {};
+    NormPart<MAX> acc[2] = {};
+    TensorRun run;
+    run.start<ROWS>(t, first, tiles);
+    grid_dependency_wait();
+    grid_dependency_launch_next();
     for (uint32_t tile = first; tile < tiles; tile += step) {
-        const uint32_t k = find_tensor(t, tile);
-        norm_tile<MAX>(t.e[k], tile - t.first_tile[k], t.tile_log2, acc);
+        if (tile >= run.end) run.seek<ROWS>(t, tile);
+        norm_tile<ROWS, MAX>(run.g, tile - run.first, t.tile_len, l2_policy(tile < t.stream_below), acc);
     }
-    reduce_block(acc, parts, kWarps);
-    if (threadIdx.x == 0u) mine = acc;
+    acc[0].join(acc[1]);
+    reduce_block(acc[0], parts, kWarps);
+    if (threadIdx.x == 0u) mine = acc[0];
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x < 32u) {
@@ -655,9 +901,11 @@ grad_cluster_kernel(const __grid_constant__ Table t, const __grid_constant__ Cli
     if constexpr (SCALE) {
         const float c = factor;
         if (!(a.in_place && c == 1.0f)) {
+            const Scaling f = {c, l2_policy(false), l2_policy(false)};
+            if (step < tiles) run.end = 0u;          // (a warp of one tile is still at its tensor)
             for (uint32_t tile = first; tile < tiles; tile += step) {
-                const uint32_t k = find_tensor(t, tile);
-                scale_tile(t.e[k], tile - t.first_tile[k], t.tile_log2, c);
+                if (tile >= run.end) run.seek<ROWS>(t, tile);
+                scale_tile<ROWS>(run.g, tile - run.first, t.tile_len, f);
             }
         }
     }
