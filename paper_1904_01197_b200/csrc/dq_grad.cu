@@ -37,13 +37,6 @@ constexpr uint64_t kEachTiles = 16384u;          // of full length
 uint32_t size_log2(uint32_t dtype) { return dtype == DQ_F32 ? 2u : 1u; }
 uint32_t element_size(uint32_t dtype) { return 1u << size_log2(dtype); }
 
-uint64_t bytes_of(const dq_tensor* list, uint32_t count)
-{
-    uint64_t bytes = 0u;
-    for (uint32_t i = 0; i < count; ++i) bytes += list[i].n << size_log2(list[i].dtype);
-    return bytes;
-}
-
 bool has_rows(const dq_tensor& t) { return t.row != 0u && t.row_stride != t.row && t.row != t.n; }
 
 dq_status check_tensor(const dq_tensor& t)
@@ -61,16 +54,22 @@ dq_status check_tensor(const dq_tensor& t)
     return DQ_OK;
 }
 
-dq_status check_list(const dq_tensor* list, uint32_t count, uint64_t* total)
+// What the checks find out about a list on the way.
+struct ListInfo {
+    uint64_t total = 0u, bytes = 0u;
+};
+
+dq_status check_list(const dq_tensor* list, uint32_t count, ListInfo* info)
 {
-    *total = 0u;
+    *info = ListInfo();
     if (count > DQ_MAX_TENSORS) return DQ_ERR_UNSUPPORTED;
     if (count != 0u && !list) return DQ_ERR_INVALID_ARG;
     for (uint32_t i = 0; i < count; ++i) {
         const dq_status s = check_tensor(list[i]);
         if (s != DQ_OK) return s;
-        *total += list[i].n;
-        if (*total >= (1ull << 34)) return DQ_ERR_UNSUPPORTED;
+        info->total += list[i].n;
+        info->bytes += list[i].n << size_log2(list[i].dtype);
+        if (info->total >= (1ull << 34)) return DQ_ERR_UNSUPPORTED;
     }
     return DQ_OK;
 }
@@ -195,12 +194,12 @@ uint32_t step_up(uint64_t len)
 // that leaves warps without a tile, and more where a warp has more than four of them, which costs it look-ups (n = 124 M
 // bf16: 2048 to 16384 elements 40 us; 25.6 M fp32: 2048 19.8 us, 4096 20.8, 1024 21.5; 25.6 M bf16: 4096 13.7, 2048 14.9; 1.7 M
 // fp32: 1024 4.1, 2048 4.4).
-uint32_t norm_tile_length(uint64_t total, uint64_t bytes, int sms)
+uint32_t norm_tile_length(const ListInfo& info, int sms)
 {
     const uint64_t warps = (uint64_t)sms * dq::kGradNormCtas * dq::kGradWarps;
-    if (total < warps * 1024u) return 1024u;
-    const uint64_t tile = bytes < 3u * total ? 4096u : 2048u;
-    return (uint32_t)(tile * (total / (warps * tile * 4u) + 1u));
+    if (info.total < warps * 1024u) return 1024u;
+    const uint64_t tile = info.bytes < 3u * info.total ? 4096u : 2048u;
+    return (uint32_t)(tile * (info.total / (warps * tile * 4u) + 1u));
 }
 
 // The tiles of the kernel that scales.  Up to two tiles of 4096 per resident warp it runs in one wave or little more, since every
@@ -229,10 +228,13 @@ uint32_t entries_of(const dq_tensor& src, const dq_tensor* dst)
     return src.n == 0u ? 0u : has_rows(src) || (dst && has_rows(*dst)) ? 2u : 1u;
 }
 
-// Fills a table from list position *next on.
+// Fills a table from list position *next on.  first_slot, where given, has a place for every tensor of the list and one more,
+// and counts tiles on from what stands at *next.
 template <int N, int W>
-void fill(dq::GradTable<N, W>& t, const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next)
+void fill(dq::GradTable<N, W>& t, const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next,
+          uint32_t* first_slot)
 {
+    const uint32_t slot = first_slot ? first_slot[*next] : 0u;
     t.count = 0u;
     t.tile_len = tile_len;
     t.stream_below = t.rows = 0u;
@@ -241,13 +243,15 @@ void fill(dq::GradTable<N, W>& t, const dq_tensor* src, const dq_tensor* dst, ui
         const uint32_t i = *next;
         const dq_tensor* to = dst ? dst + i : nullptr;
         const uint32_t entries = entries_of(src[i], to);
-        if (entries == 0u) continue;
         if (t.count + entries > (uint32_t)N) break;
+        if (first_slot) first_slot[i + 1u] = slot + tiles;
+        if (entries == 0u) continue;
         const Walk w = walk_of(src[i], to);
         const uint64_t s = reinterpret_cast<uintptr_t>(src[i].data), n = src[i].n;
         dq::GradEntry<W>& e = t.e[t.count];
         t.first_tile[t.count++] = tiles;
         tiles += tiles_of(n, w, tile_len);
+        if (first_slot) first_slot[i + 1u] = slot + tiles;
         e.w[0] = (uint32_t)s;
         e.w[1] = (uint32_t)(s >> 32) | (uint32_t)src[i].dtype << 25 | w.walk << 27 | (uint32_t)(n >> 32) << 29;
         e.w[2] = (uint32_t)n;
@@ -273,30 +277,31 @@ uint32_t grid_for(uint32_t tiles, uint32_t warps, uint32_t most)
     return std::max(1u, std::min((tiles + warps - 1u) / warps, most));
 }
 
-uint64_t entries_in(const dq_tensor* src, const dq_tensor* dst, uint32_t count)
+bool entries_fit(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t most)
 {
-    uint64_t entries = 0u;
-    for (uint32_t i = 0; i < count; ++i) entries += entries_of(src[i], dst ? dst + i : nullptr);
-    return entries;
+    uint32_t entries = 0u;
+    for (uint32_t i = 0; i < count && entries <= most; ++i) entries += entries_of(src[i], dst ? dst + i : nullptr);
+    return entries <= most;
 }
 
 // Calls f(table) with the smallest table that holds the rest of the list.
 template <int W, class F>
-cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next, F&& f)
+cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next,
+                       uint32_t* first_slot, F&& f)
 {
-    const uint64_t left = entries_in(src + *next, dst ? dst + *next : nullptr, count - *next);
-    if (left <= (uint64_t)kSmall<W>) {
+    const dq_tensor* to = dst ? dst + *next : nullptr;
+    if (entries_fit(src + *next, to, count - *next, kSmall<W>)) {
         dq::GradTable<kSmall<W>, W> t;
-        fill(t, src, dst, count, tile_len, next);
+        fill(t, src, dst, count, tile_len, next, first_slot);
         return f(t);
     }
-    if (left <= (uint64_t)kMiddle<W>) {
+    if (entries_fit(src + *next, to, count - *next, kMiddle<W>)) {
         dq::GradTable<kMiddle<W>, W> t;
-        fill(t, src, dst, count, tile_len, next);
+        fill(t, src, dst, count, tile_len, next, first_slot);
         return f(t);
     }
     dq::GradTable<kLarge<W>, W> t;
-    fill(t, src, dst, count, tile_len, next);
+    fill(t, src, dst, count, tile_len, next, first_slot);
     return f(t);
 }
 
@@ -363,11 +368,11 @@ cudaError_t launch_cluster(const Table& t, const dq::ClipArgs& a, cudaStream_t s
 // The parts of the norm of a list into slots; *num_slots counts them.
 template <bool MAX, bool EACH>
 cudaError_t launch_parts(const dq_tensor* list, uint32_t count, uint32_t tile_len, int sms, uint64_t keep,
-                         dq::NormPart<MAX>* slots, uint32_t* num_slots, cudaStream_t st)
+                         dq::NormPart<MAX>* slots, uint32_t* num_slots, uint32_t* first_slot, cudaStream_t st)
 {
     *num_slots = 0u;
     for (uint32_t next = 0u; next < count;) {
-        const cudaError_t e = with_table<kNorm>(list, nullptr, count, tile_len, &next, [&](auto& t) {
+        const cudaError_t e = with_table<kNorm>(list, nullptr, count, tile_len, &next, first_slot, [&](auto& t) {
             using Table = std::remove_reference_t<decltype(t)>;
             const uint32_t tiles = t.first_tile[t.count];
             if (tiles == 0u) return cudaSuccess;
@@ -407,25 +412,22 @@ cudaError_t launch_join(const dq::NormPart<MAX>* slots, uint32_t num_slots, floa
     return launch_join<MAX>(none, slots, num_slots, out_norm, nullptr, status, st);
 }
 
-// The same with the norms of single tensors, after launch_parts<MAX, true>.
+// The same with the norms of single tensors: tensor i has the slots from first_slot[i] to first_slot[i + 1].
 template <bool MAX>
-cudaError_t launch_join_each(const dq_tensor* list, uint32_t count, uint32_t tile_len, const dq::NormPart<MAX>* slots,
-                             uint32_t num_slots, float* out_norm, float* out_norms, uint32_t* status, cudaStream_t st)
+cudaError_t launch_join_each(uint32_t count, const uint32_t* first_slot, const dq::NormPart<MAX>* slots, uint32_t num_slots,
+                             float* out_norm, float* out_norms, uint32_t* status, cudaStream_t st)
 {
-    uint32_t slot = 0u, i = 0u;
+    uint32_t done = 0u;
     auto launch = [&](auto& t) {
-        const uint32_t begin = i;
-        t.count = 0u;
-        t.first[0] = slot;
-        for (; i < count && t.count < (uint32_t)t.kCapacity; ++i) {
-            if (list[i].n) slot += tiles_of(list[i].n, walk_of(list[i], nullptr), tile_len);
-            t.first[++t.count] = slot;
-        }
-        return launch_join<MAX>(t, slots, num_slots, begin == 0u ? out_norm : nullptr, out_norms + begin, status, st);
+        t.count = std::min(count - done, (uint32_t)t.kCapacity);
+        std::copy_n(first_slot + done, t.count + 1u, t.first);
+        const cudaError_t e = launch_join<MAX>(t, slots, num_slots, done == 0u ? out_norm : nullptr, out_norms + done, status, st);
+        done += t.count;
+        return e;
     };
     cudaError_t e = cudaSuccess;
-    while (i < count && e == cudaSuccess) {
-        if (count - i <= (uint32_t)kEachMiddle) {
+    while (done < count && e == cudaSuccess) {
+        if (count - done <= (uint32_t)kEachMiddle) {
             dq::GradEachTable<kEachMiddle> t;
             e = launch(t);
         } else {
@@ -437,44 +439,59 @@ cudaError_t launch_join_each(const dq_tensor* list, uint32_t count, uint32_t til
 }
 
 template <bool MAX>
-dq_status norm_of(const dq_tensor* list, uint32_t count, uint64_t total, float* out_norm, float* out_norms, uint32_t* status,
-                  void* workspace, cudaStream_t st)
+dq_status norm_of(const dq_tensor* list, uint32_t count, const ListInfo& info, float* out_norm, float* out_norms,
+                  uint32_t* status, void* workspace, cudaStream_t st)
 {
     const int sms = dq::device_sm_count();
     if (sms <= 0) return DQ_ERR_CUDA;
     auto* slots = static_cast<dq::NormPart<MAX>*>(workspace);
-    const uint64_t bytes = bytes_of(list, count);
     uint32_t num_slots = 0u;
     cudaError_t e;
     if (out_norms && count) {
+        std::unique_ptr<uint32_t[]> first_slot(new (std::nothrow) uint32_t[count + 1u]);
+        if (!first_slot) return DQ_ERR_CUDA;
+        first_slot[0] = 0u;
         // (no more slots than the workspace has)
-        const uint32_t tile_len = std::max(norm_tile_length(total, bytes, sms), step_up(total / kEachTiles + 1u));
-        e = launch_parts<MAX, true>(list, count, tile_len, sms, ~0ull, slots, &num_slots, st);
+        const uint32_t tile_len = std::max(norm_tile_length(info, sms), step_up(info.total / kEachTiles + 1u));
+        e = launch_parts<MAX, true>(list, count, tile_len, sms, ~0ull, slots, &num_slots, first_slot.get(), st);
         if (e == cudaSuccess)
-            e = launch_join_each<MAX>(list, count, tile_len, slots, num_slots, out_norm, out_norms, status, st);
-    } else if (is_short(count, total)) {
+            e = launch_join_each<MAX>(count, first_slot.get(), slots, num_slots, out_norm, out_norms, status, st);
+    } else if (is_short(count, info.total)) {
         dq::ClipArgs a = {};
         a.out_norm = out_norm;
         a.status = status;
         uint32_t next = 0u;
-        e = with_table<kNorm>(list, nullptr, count, cluster_tile_length(total, count), &next,
+        e = with_table<kNorm>(list, nullptr, count, cluster_tile_length(info.total, count), &next, nullptr,
                               [&](const auto& t) { return launch_cluster<MAX, false>(t, a, st); });
     } else {
-        e = launch_parts<MAX, false>(list, count, norm_tile_length(total, bytes, sms), sms, ~0ull, slots, &num_slots, st);
+        e = launch_parts<MAX, false>(list, count, norm_tile_length(info, sms), sms, ~0ull, slots, &num_slots, nullptr, st);
         if (e == cudaSuccess) e = launch_join<MAX>(slots, num_slots, out_norm, status, st);
     }
     return e == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
 }
 
-// src[i] * c into dst[i]; the norm is that of norm_list, which is the same elements.
+// A list that is clipped: src[i] * c into dst[i].  The norm is that of norm_list, which is the same elements; `info` is about it.
+struct Job {
+    const dq_tensor *src, *dst;
+    uint32_t count;
+    const dq_tensor* norm_list;
+    uint32_t norm_count;
+    ListInfo info;
+    const dq_clip* clip;         // null: nothing is clipped
+    bool in_place;
+};
+
 template <bool MAX>
-dq_status scale(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint64_t total, const dq_tensor* norm_list,
-                uint32_t norm_count, const dq_clip* clip, bool in_place, void* workspace, cudaStream_t st)
+dq_status scale(const Job& job, void* workspace, cudaStream_t st)
 {
     const int sms = dq::device_sm_count();
     if (sms <= 0) return DQ_ERR_CUDA;
+    const dq_tensor *src = job.src, *dst = job.dst;
+    const uint32_t count = job.count;
+    const ListInfo& info = job.info;
+    const dq_clip* clip = job.clip;
     dq::ClipArgs a = {};
-    a.in_place = in_place ? 1u : 0u;
+    a.in_place = job.in_place ? 1u : 0u;
     a.max_kind = MAX ? 1u : 0u;
     a.stream = 1u;
     a.max_norm = clip ? clip->max_norm : 0.0f;
@@ -485,18 +502,18 @@ dq_status scale(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint
         a.status = clip->status_word;
     }
     if (clip && !clip->norm) {
-        if (is_short(count, total)) {
-            const cudaError_t e = with_table<kScale>(src, dst, count, cluster_tile_length(total, count), &next,
+        if (is_short(count, info.total)) {
+            const cudaError_t e = with_table<kScale>(src, dst, count, cluster_tile_length(info.total, count), &next, nullptr,
                                                      [&](const auto& t) { return launch_cluster<MAX, true>(t, a, st); });
             return e == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
         }
         auto* slots = reinterpret_cast<dq::NormPart<MAX>*>(static_cast<char*>(workspace) + 16);
-        const uint64_t bytes = bytes_of(norm_list, norm_count);
-        cudaError_t e = launch_parts<MAX, false>(norm_list, norm_count, norm_tile_length(total, bytes, sms), sms,
-                                                kKeepBytes * total / bytes, slots, &a.num_slots, st);
+        const uint64_t keep = info.bytes ? kKeepBytes * info.total / info.bytes : 0u;
+        cudaError_t e = launch_parts<MAX, false>(job.norm_list, job.norm_count, norm_tile_length(info, sms), sms, keep, slots,
+                                                 &a.num_slots, nullptr, st);
         if (e != cudaSuccess) return DQ_ERR_CUDA;
         a.slots = slots;
-        if (entries_in(src, dst, count) > (uint64_t)kLarge<kScale>) {
+        if (!entries_fit(src, dst, count, kLarge<kScale>)) {
             // several launches follow: they take the norm itself
             float* norm = a.out_norm ? a.out_norm : static_cast<float*>(workspace);
             if (launch_join<MAX>(slots, a.num_slots, norm, a.status, st) != cudaSuccess) return DQ_ERR_CUDA;
@@ -506,10 +523,10 @@ dq_status scale(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint
             a.status = nullptr;
         }
     }
-    const uint32_t tile_len = scale_tile_length(total, sms);
+    const uint32_t tile_len = scale_tile_length(info.total, sms);
     bool first = true;
     while (next < count || first) {
-        const cudaError_t e = with_table<kScale>(src, dst, count, tile_len, &next, [&](const auto& t) {
+        const cudaError_t e = with_table<kScale>(src, dst, count, tile_len, &next, nullptr, [&](const auto& t) {
             using Table = std::remove_cv_t<std::remove_reference_t<decltype(t)>>;
             const uint32_t tiles = t.first_tile[t.count];
             if (tiles == 0u && !(first && (a.out_norm || a.status))) return cudaSuccess;
@@ -536,27 +553,30 @@ dq_status check_clip(const dq_clip* clip)
     return DQ_OK;
 }
 
-dq_status check_workspace(const dq_tensor* list, uint32_t count, int each, const void* workspace, uint64_t bytes)
+uint64_t workspace_bytes_for(uint32_t count, const ListInfo& info, bool each)
 {
-    const uint64_t need = dq_grad_workspace_bytes(list, count, each);
+    if (!each && is_short(count, info.total)) return 0u;
+    // (tiles of a tensor in rows may be half as long, and every tensor may have two that are short)
+    const uint64_t slots = each ? 2u * kEachTiles + kEachTiles / 8u + 2u * (uint64_t)count
+                                : (uint64_t)kMaxGrid * (2u * (uint64_t)count / (uint64_t)(kLarge<kNorm> - 1) + 1u);
+    return (16u + 8u * slots + 255u) / 256u * 256u;
+}
+
+dq_status check_workspace(uint64_t need, const void* workspace, uint64_t bytes)
+{
     if (need == 0u) return DQ_OK;
     if (!workspace || bytes < need) return DQ_ERR_INVALID_ARG;
     return (reinterpret_cast<uintptr_t>(workspace) & 15u) == 0u ? DQ_OK : DQ_ERR_ALIGNMENT;
 }
 
-// The checks and the launch that clip, gather and scatter share.  `list` is the list of tensors (the other side of gather
-// and scatter is `flat`, cut into tensors of the list's sizes).
-dq_status scale_checked(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint64_t total, const dq_tensor* list,
-                        const dq_tensor* norm_list, uint32_t norm_count, const dq_clip* clip, bool in_place, void* workspace,
-                        uint64_t workspace_bytes, cudaStream_t st)
+// The last check and the launch that clip, gather and scatter share.
+dq_status scale_checked(const Job& job, void* workspace, uint64_t workspace_bytes, cudaStream_t st)
 {
-    if (clip && !clip->norm) {
-        const dq_status s = check_workspace(list, count, 0, workspace, workspace_bytes);
+    if (job.clip && !job.clip->norm) {
+        const dq_status s = check_workspace(workspace_bytes_for(job.count, job.info, false), workspace, workspace_bytes);
         if (s != DQ_OK) return s;
     }
-    if (clip && clip->kind == DQ_NORM_MAX)
-        return scale<true>(src, dst, count, total, norm_list, norm_count, clip, in_place, workspace, st);
-    return scale<false>(src, dst, count, total, norm_list, norm_count, clip, in_place, workspace, st);
+    return job.clip && job.clip->kind == DQ_NORM_MAX ? scale<true>(job, workspace, st) : scale<false>(job, workspace, st);
 }
 
 // The slices of a flat vector that belong to the tensors of a list.
@@ -587,41 +607,37 @@ extern "C" {
 
 uint64_t dq_grad_workspace_bytes(const dq_tensor* list, uint32_t count, int each)
 {
-    uint64_t total;
-    if (check_list(list, count, &total) != DQ_OK || (!each && is_short(count, total))) return 0u;
-    // (tiles of a tensor in rows may be half as long, and every tensor may have two that are short)
-    const uint64_t slots = each ? 2u * kEachTiles + kEachTiles / 8u + 2u * (uint64_t)count
-                                : (uint64_t)kMaxGrid * (2u * (uint64_t)count / (uint64_t)(kLarge<kNorm> - 1) + 1u);
-    return (16u + 8u * slots + 255u) / 256u * 256u;
+    ListInfo info;
+    return check_list(list, count, &info) == DQ_OK ? workspace_bytes_for(count, info, each != 0) : 0u;
 }
 
 dq_status dq_grad_norm(const dq_tensor* grads, uint32_t count, dq_norm kind, float* out_norm, float* out_norms,
                        uint32_t* status_word, void* workspace, uint64_t workspace_bytes, void* cuda_stream)
 {
-    uint64_t total;
-    dq_status s = check_list(grads, count, &total);
+    ListInfo info;
+    dq_status s = check_list(grads, count, &info);
     if (s != DQ_OK) return s;
     if (!out_norm || (kind != DQ_NORM_L2 && kind != DQ_NORM_MAX)) return DQ_ERR_INVALID_ARG;
     for (const void* p : {(const void*)out_norm, (const void*)out_norms, (const void*)status_word})
         if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0u) return DQ_ERR_ALIGNMENT;
-    s = check_workspace(grads, count, out_norms != nullptr, workspace, workspace_bytes);
+    s = check_workspace(workspace_bytes_for(count, info, out_norms != nullptr), workspace, workspace_bytes);
     if (s != DQ_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return kind == DQ_NORM_MAX ? norm_of<true>(grads, count, total, out_norm, out_norms, status_word, workspace, st)
-                               : norm_of<false>(grads, count, total, out_norm, out_norms, status_word, workspace, st);
+    return kind == DQ_NORM_MAX ? norm_of<true>(grads, count, info, out_norm, out_norms, status_word, workspace, st)
+                               : norm_of<false>(grads, count, info, out_norm, out_norms, status_word, workspace, st);
 }
 
 dq_status dq_grad_clip(const dq_tensor* grads, uint32_t count, const dq_clip* clip, const dq_tensor* out, void* workspace,
                        uint64_t workspace_bytes, void* cuda_stream)
 {
-    uint64_t total, out_total;
-    dq_status s = check_list(grads, count, &total);
+    ListInfo info, out_info;
+    dq_status s = check_list(grads, count, &info);
     if (s != DQ_OK) return s;
     if (!clip) return DQ_ERR_INVALID_ARG;
     s = check_clip(clip);
     if (s != DQ_OK) return s;
     if (out) {
-        s = check_list(out, count, &out_total);
+        s = check_list(out, count, &out_info);
         if (s != DQ_OK) return s;
         for (uint32_t i = 0; i < count; ++i) {
             if (out[i].n != grads[i].n) return DQ_ERR_INVALID_ARG;
@@ -630,43 +646,44 @@ dq_status dq_grad_clip(const dq_tensor* grads, uint32_t count, const dq_clip* cl
     }
     s = out ? check_outputs(grads, count, out, count, clip) : check_outputs(nullptr, 0u, grads, count, clip);
     if (s != DQ_OK) return s;
-    return scale_checked(grads, out ? out : grads, count, total, grads, grads, count, clip, out == nullptr, workspace,
-                         workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+    return scale_checked({grads, out ? out : grads, count, grads, count, info, clip, out == nullptr}, workspace, workspace_bytes,
+                         static_cast<cudaStream_t>(cuda_stream));
 }
 
 dq_status dq_grad_gather(const dq_tensor* grads, uint32_t count, const dq_clip* clip, float* out_flat, void* workspace,
                          uint64_t workspace_bytes, void* cuda_stream)
 {
-    uint64_t total;
-    dq_status s = check_list(grads, count, &total);
+    ListInfo info;
+    dq_status s = check_list(grads, count, &info);
     if (s != DQ_OK) return s;
     if (clip && (s = check_clip(clip)) != DQ_OK) return s;
-    if (total != 0u && !out_flat) return DQ_ERR_INVALID_ARG;
+    if (info.total != 0u && !out_flat) return DQ_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(out_flat) & 15u) != 0u) return DQ_ERR_ALIGNMENT;
-    const dq_tensor flat = {out_flat, total, 0u, 0u, DQ_F32, 0u};
+    const dq_tensor flat = {out_flat, info.total, 0u, 0u, DQ_F32, 0u};
     s = check_outputs(grads, count, &flat, 1u, clip);
     if (s != DQ_OK) return s;
     Slices to;
     if (!to.cut(out_flat, grads, count)) return DQ_ERR_CUDA;
-    return scale_checked(grads, to.t, count, total, grads, grads, count, clip, false, workspace, workspace_bytes,
+    return scale_checked({grads, to.t, count, grads, count, info, clip, false}, workspace, workspace_bytes,
                          static_cast<cudaStream_t>(cuda_stream));
 }
 
 dq_status dq_grad_scatter(const float* flat, const dq_clip* clip, const dq_tensor* out, uint32_t count, void* workspace,
                           uint64_t workspace_bytes, void* cuda_stream)
 {
-    uint64_t total;
-    dq_status s = check_list(out, count, &total);
+    ListInfo info;
+    dq_status s = check_list(out, count, &info);
     if (s != DQ_OK) return s;
     if (clip && (s = check_clip(clip)) != DQ_OK) return s;
-    if (total != 0u && !flat) return DQ_ERR_INVALID_ARG;
+    if (info.total != 0u && !flat) return DQ_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(flat) & 15u) != 0u) return DQ_ERR_ALIGNMENT;
-    const dq_tensor whole = {const_cast<float*>(flat), total, 0u, 0u, DQ_F32, 0u};
+    const dq_tensor whole = {const_cast<float*>(flat), info.total, 0u, 0u, DQ_F32, 0u};
     s = check_outputs(&whole, 1u, out, count, clip);
     if (s != DQ_OK) return s;
     Slices from;
     if (!from.cut(flat, out, count)) return DQ_ERR_CUDA;
-    return scale_checked(from.t, out, count, total, out, &whole, 1u, clip, false, workspace, workspace_bytes,
+    info.bytes = 4u * info.total;
+    return scale_checked({from.t, out, count, &whole, 1u, info, clip, false}, workspace, workspace_bytes,
                          static_cast<cudaStream_t>(cuda_stream));
 }
 
