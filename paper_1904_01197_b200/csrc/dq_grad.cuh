@@ -325,6 +325,29 @@ __device__ __forceinline__ uint32_t narrow(float a, float b, uint32_t type)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The elements of a lane that lie 32 apart in a tensor of loose rows, several in flight; 0 from `end` on.
+constexpr uint32_t kGradLooseFlight = 16;
+
+template <bool F32>
+__device__ __forceinline__ void load_loose(float (&x)[kGradLooseFlight], const char* src, uint32_t type, uint32_t v, uint32_t end,
+                                           RowCursor& cur)
+{
+    uint32_t w[kGradLooseFlight];
+#pragma unroll
+    for (uint32_t j = 0; j < kGradLooseFlight; ++j) {
+        w[j] = 0u;
+        if (v + 32u * j < end) {
+            if constexpr (F32)
+                w[j] = reinterpret_cast<const uint32_t*>(src)[cur.at];
+            else
+                w[j] = reinterpret_cast<const uint16_t*>(src)[cur.at];
+        }
+        cur.next();
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kGradLooseFlight; ++j) x[j] = F32 ? __uint_as_float(w[j]) : widen(w[j], type).x;
+}
+
 // ------------------------------------------------------------------------------------------ norm
 // A lane's part of a norm: the sum of squares in fp64, or the largest bit pattern without the sign.
 template <bool MAX> struct NormPart;
@@ -455,10 +478,11 @@ __device__ __forceinline__ void norm_tile(const GradTensor& g, uint32_t index, u
             });
         } else {
             RowCursor cur(s.start + lane, 32u, g.row, g.src_stride);
-#pragma unroll 4
-            for (uint32_t v = lane; v < s.hi; v += 32u) {
-                acc[0].add(load_element(g.src, cur.at, g.src_type));
-                cur.next();
+            for (uint32_t v = lane; v < s.hi; v += 32u * kGradLooseFlight) {
+                float x[kGradLooseFlight];
+                load_loose<F32>(x, g.src, g.src_type, v, s.hi, cur);
+#pragma unroll
+                for (uint32_t j = 0; j < kGradLooseFlight; ++j) acc[j & 1u].add(x[j]);
             }
         }
     }
@@ -562,8 +586,7 @@ struct ClipArgs {
     float* out_norm;             // optional
     uint32_t* status;            // optional
     uint16_t in_place;           // the destination is the source
-    uint8_t max_kind;            // the slots are maxima
-    uint8_t stream;              // the destination is not wanted in L2 for long
+    uint16_t max_kind;           // the slots are maxima
 };
 
 __device__ __forceinline__ float clip_factor(float norm, float max_norm)
@@ -766,11 +789,14 @@ __device__ __forceinline__ void scale_tile(const GradTensor& g, uint32_t index, 
             scale_row_groups<SF32, DF32>(s, g, f);
         } else {
             RowCursor from(s.start + lane, 32u, g.row, g.src_stride), to(s.start + lane, 32u, g.row, g.dst_stride);
-#pragma unroll 4
-            for (uint32_t v = lane; v < s.hi; v += 32u) {
-                store_element(g.dst, to.at, g.dst_type, __fmul_rn(load_element(g.src, from.at, g.src_type), f.c));
-                from.next();
-                to.next();
+            for (uint32_t v = lane; v < s.hi; v += 32u * kGradLooseFlight) {
+                float x[kGradLooseFlight];
+                load_loose<SF32>(x, g.src, g.src_type, v, s.hi, from);
+#pragma unroll
+                for (uint32_t j = 0; j < kGradLooseFlight; ++j) {
+                    if (v + 32u * j < s.hi) store_element(g.dst, to.at, g.dst_type, __fmul_rn(x[j], f.c));
+                    to.next();
+                }
             }
         }
     }
@@ -844,7 +870,7 @@ grad_scale_kernel(const __grid_constant__ Table t, const __grid_constant__ ClipA
     }
     grid_dependency_launch_next();
     if (a.in_place && c == 1.0f) return;
-    const Scaling f = {c, l2_policy(true), l2_policy(a.stream != 0u)};
+    const Scaling f = {c, l2_policy(true), l2_policy(true)};
     for (uint32_t i = first; i < tiles; i += gridDim.x * kGradWarps) {
         const uint32_t tile = tiles - 1u - i;
         if (tile < run.first || tile >= run.end) run.seek<ROWS>(t, tile);
@@ -877,8 +903,8 @@ grad_cluster_kernel(const __grid_constant__ Table t, const __grid_constant__ Cli
     acc[0].join(acc[1]);
     reduce_block(acc[0], parts, kWarps);
     if (threadIdx.x == 0u) mine = acc[0];
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     if (threadIdx.x < 32u) {
         NormPart<MAX> all = {};
         if (threadIdx.x < gridDim.x) {
@@ -897,7 +923,7 @@ grad_cluster_kernel(const __grid_constant__ Table t, const __grid_constant__ Cli
         }
     }
     __syncthreads();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");     // (no CTA leaves while its part is read)
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");     // (no CTA leaves while its part is read)
     if constexpr (SCALE) {
         const float c = factor;
         if (!(a.in_place && c == 1.0f)) {
@@ -909,7 +935,7 @@ grad_cluster_kernel(const __grid_constant__ Table t, const __grid_constant__ Cli
             }
         }
     }
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 }  // namespace dq

@@ -219,6 +219,13 @@ def test_norms_of_empty_lists(dq):
     flat = torch.full((1,), 9.0, device="cuda")
     dq.grad_gather([e], flat, max_norm=1.0, out_norm=out.fill_(9.0))
     assert float(out) == 0.0 and float(flat) == 9.0
+    many = [e] * 300                                     # more than a short list's tables hold
+    for call in (lambda: dq.grad_norm(many, out_norm=out), lambda: dq.grad_clip(many, 1.0, out=many, out_norm=out),
+                 lambda: dq.grad_clip(many, 1.0, out_norm=out), lambda: dq.grad_gather(many, flat, max_norm=1.0, out_norm=out),
+                 lambda: dq.grad_scatter(e, many, max_norm=1.0, kind=dq.DQ_NORM_MAX, out_norm=out)):
+        out.fill_(9.0)
+        call()
+        assert float(out) == 0.0
     given = torch.full((1,), 4.0, device="cuda")
     assert float(dq.grad_clip([e], 1.0, norm=given, out_norm=out)) == 4.0
 
@@ -336,7 +343,8 @@ def _blocks(dtype, rows, widths, total, seed=1, lead=()):
 @pytest.mark.parametrize("pair", [(F32, F32), (BF16, BF16), (F16, F32), (F32, BF16)], ids=str)
 @pytest.mark.parametrize("shape", [(1, [8, 8], 16), (37, [8, 16, 24], 48), (37, [8, 16, 24], 53), (50, [1, 2, 33, 7], 50),
                                    (3000, [1], 700), (700, [512, 512, 512], 1536), (300, [1000, 999], 2000),
-                                   (9, [5000], 9000), (2, [200_000], 300_001)], ids=str)
+                                   (9, [5000], 9000), (2, [200_000], 300_001), (40, [600, 511, 513], 1624),
+                                   (60, [511, 512], 1024), (5, [2041, 2042, 4096], 9001), (1200, [5] * 150, 800)], ids=str)
 def test_column_blocks(dq, shape, pair):
     rows, widths, total = shape
     m, blocks = _blocks(pair[0], rows, widths, total)
@@ -383,6 +391,26 @@ def _split(m, widths):
         out.append(m[..., at:at + w])
         at += w
     return out
+
+
+@pytest.mark.parametrize("which", [F32, BF16], ids=["f32", "bf16"])
+def test_more_column_blocks_than_a_table_holds(dq, which):
+    widths = [8 + i % 40 for i in range(1100)]
+    m, blocks = _blocks(which, 12, widths, sum(widths) + 9, seed=3)
+    before, ref = m.clone(), [b.contiguous().clone() for b in blocks]
+    _, total = _norms([_f64(b) for b in ref], "l2")
+    limit = float(np.float32(0.25 * total))
+    norms = torch.empty(len(blocks), device="cuda")
+    _assert_norm(dq.grad_norm(blocks, out_norms=norms), total, "l2")
+    for v, r in zip(norms.tolist(), ref):
+        _assert_norm(v, _norms([_f64(r)], "l2")[1], "l2")
+    out = [torch.empty(b.shape, device="cuda") for b in blocks]
+    norm = dq.grad_clip(blocks, limit, out=out)
+    _assert_norm(norm, total, "l2")
+    _assert_clipped(out, ref, norm, limit, total)
+    norm = dq.grad_clip(blocks, limit)
+    _assert_clipped([b.contiguous() for b in blocks], ref, norm, limit, total)
+    assert torch.equal(m[:, sum(widths):], before[:, sum(widths):])
 
 
 def test_other_layouts(dq):
