@@ -156,6 +156,31 @@ def test_tensors_that_overlap_are_refused(dq):
         assert L.dq_grad_scatter(BASE + at, None, flat, 2, None, 0, None) == INVALID
 
 
+@pytest.mark.parametrize("order", ["ascending", "descending", "two_runs", "random"])
+@pytest.mark.parametrize("count", [100, 300, 3000])
+def test_one_overlap_among_many_tensors_is_found(dq, count, order):
+    import random
+    rng = random.Random(count)
+    spots = list(range(2 * count))
+    if order == "descending":
+        spots.reverse()
+    elif order == "two_runs":
+        spots = spots[::2] + spots[1::2]
+    elif order == "random":
+        rng.shuffle(spots)
+    n = 8192                                            # (long lists: the workspace's fault stops a call that has no other)
+    tensors = [_t(dq, data=BASE + 4 * n * s, n=n) for s in spots]
+    assert count * n > 1 << 19
+    assert _clip_status(dq, tensors[:count], tensors[count:]) == NO_OVERLAP
+    for _ in range(5):
+        k = rng.randrange(count, 2 * count)
+        if spots[k] == 2 * count - 1:
+            continue
+        bad = list(tensors)
+        bad[k] = _t(dq, data=BASE + 4 * n * spots[k] + 16, n=n)          # 16 bytes into the next one
+        assert _clip_status(dq, bad[:count], bad[count:]) == INVALID
+
+
 def test_workspace_sizes(dq):
     L = dq.lib()
     short, long = _list(dq, _t(dq, n=4096)), _list(dq, _t(dq))
