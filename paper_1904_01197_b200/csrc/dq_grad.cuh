@@ -542,6 +542,23 @@ grad_norm_kernel(const __grid_constant__ Table t, NormPart<MAX>* slots)
     }
 }
 
+// Joins the slots begin, begin + step, ... below end: F of them are in flight together.
+template <uint32_t F, bool MAX>
+__device__ __forceinline__ void join_slots(NormPart<MAX>& acc, const NormPart<MAX>* slots, uint32_t begin, uint32_t end,
+                                           uint32_t step)
+{
+    for (uint32_t i = begin; i < end; i += F * step) {
+        NormPart<MAX> part[F];
+#pragma unroll
+        for (uint32_t j = 0; j < F; ++j) {
+            part[j] = slots[min(i + j * step, end - 1u)];
+            if (i + j * step >= end) part[j] = {};
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < F; ++j) acc.join(part[j]);
+    }
+}
+
 // The whole from the slots of all launches before it (CTA 0, where `out_norm` is given), and the norms of single tensors
 // from the slots of their tiles, a warp each: tensor i of the launch owns the slots [first[i], first[i + 1]).
 constexpr int kGradJoinThreads = 1024;
@@ -564,14 +581,14 @@ grad_norm_join_kernel(const __grid_constant__ Table t, const NormPart<MAX>* slot
     NormPart<MAX> acc = {};
     if (blockIdx.x == 0u) {
         if (!out_norm) return;
-        for (uint32_t i = threadIdx.x; i < num_slots; i += kGradJoinThreads) acc.join(slots[i]);
+        join_slots<8>(acc, slots, threadIdx.x, num_slots, kGradJoinThreads);
         reduce_block(acc, parts, kGradJoinThreads / 32);
         if (threadIdx.x == 0u) publish_norm(acc.norm(), out_norm, status);
         return;
     }
     const uint32_t i = (blockIdx.x - 1u) * (kGradJoinThreads / 32u) + (threadIdx.x >> 5);
     if (i >= t.count) return;
-    for (uint32_t k = t.first[i] + (threadIdx.x & 31u); k < t.first[i + 1u]; k += 32u) acc.join(slots[k]);
+    join_slots<16>(acc, slots, t.first[i] + (threadIdx.x & 31u), t.first[i + 1u], 32u);
     reduce_warp(acc);
     if ((threadIdx.x & 31u) == 0u) out_norms[i] = acc.norm();
 }
@@ -826,19 +843,8 @@ __device__ __forceinline__ void scale_tile(const GradTensor& g, uint32_t tile, u
 template <bool MAX>
 __device__ __forceinline__ float joined_norm(const ClipArgs& a)
 {
-    constexpr uint32_t kFlight = 20;
-    const NormPart<MAX>* slots = static_cast<const NormPart<MAX>*>(a.slots);
     NormPart<MAX> acc = {};
-    for (uint32_t i = threadIdx.x & 31u; i < a.num_slots; i += 32u * kFlight) {
-        NormPart<MAX> part[kFlight];
-#pragma unroll
-        for (uint32_t j = 0; j < kFlight; ++j) {
-            part[j] = slots[min(i + 32u * j, a.num_slots - 1u)];
-            if (i + 32u * j >= a.num_slots) part[j] = {};
-        }
-#pragma unroll
-        for (uint32_t j = 0; j < kFlight; ++j) acc.join(part[j]);
-    }
+    join_slots<20>(acc, static_cast<const NormPart<MAX>*>(a.slots), threadIdx.x & 31u, a.num_slots, 32u);
     reduce_warp(acc);
     return acc.norm();
 }
