@@ -293,7 +293,7 @@ typedef struct {
     void*    data;        /* device; not written where the tensor is an input; may be NULL when n = 0          */
     uint64_t n;           /* elements                                                                         */
     uint64_t row;         /* elements per row, a divisor of n below 2^31; 0: contiguous                        */
-    uint64_t row_stride;  /* row <= row_stride < 2^32; ignored when row = 0                                    */
+    uint64_t row_stride;  /* row <= row_stride < 2^32; ignored when row = 0 or the rows are contiguous          */
     dq_dtype dtype;
     uint32_t reserved;    /* 0                                                                                */
 } dq_tensor;
@@ -321,7 +321,7 @@ typedef struct {
 
 /*
  * Device memory that the calls below want as `workspace` for this list (the input list; dq_grad_scatter: the outputs),
- * 16-byte aligned; 0 for short lists, where it may be NULL.  It holds nothing between calls; calls that may overlap in
+ * 16-byte aligned; 0 for short lists, where it may be NULL (as in calls that compute no norm).  It holds nothing between calls; calls that may overlap in
  * time need one each.  each != 0: for dq_grad_norm with out_norms.  0 also for a list that the calls refuse.
  */
 uint64_t dq_grad_workspace_bytes(const dq_tensor* list, uint32_t count, int each);

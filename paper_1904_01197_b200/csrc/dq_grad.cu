@@ -27,8 +27,10 @@ static_assert(sizeof(dq::GradTable<kLarge<kScale>, kScale>) + sizeof(dq::ClipArg
 constexpr int kEachMiddle = 512, kEachLarge = 8000;          // tables of the single tensors' slots, 4 bytes each
 static_assert(sizeof(dq::GradEachTable<kEachLarge>) + 64 <= 32764, "kernel parameters");
 
-// Lists up to this many elements (and half of kMiddle tensors) are done by one cluster in one launch.
-constexpr uint64_t kShortElements = 1ull << 19;
+// Lists up to this many elements (and half of kMiddle tensors) are done by one cluster in one launch.  Where the GPU is through
+// sooner with two launches (norm, from 200,000 elements on: 524,288 3.8 us and 5.9 with the cluster; norm and scaling 4.8 and 8.2,
+// 262,144 4.8 and 5.9), it still waits for the host, whose work is 4 us for one launch and 7.3 for two.
+constexpr uint64_t kShortNorm = 1ull << 19, kShortScale = 3ull << 17;
 
 // Parts of the norm: at most kMaxGrid of a launch, or one per tile where each tensor's norm is wanted as well.
 constexpr uint32_t kMaxGrid = 1024u;
@@ -67,7 +69,9 @@ dq_status check_tensor(const dq_tensor& t)
     if (reinterpret_cast<uintptr_t>(t.data) >> 57) return DQ_ERR_UNSUPPORTED;           // (no device address is as large)
     if (t.row != 0u) {
         if (t.n % t.row != 0u || t.row_stride < t.row) return DQ_ERR_INVALID_ARG;
-        if (has_rows(t) && (t.row >= (1ull << 31) || t.row_stride >= (1ull << 32))) return DQ_ERR_UNSUPPORTED;
+        if (has_rows(t) && (t.row >= (1ull << 31) || t.row_stride >= (1ull << 32) ||
+                            t.n / t.row > (1ull << 57) / (t.row_stride << size_log2(t.dtype))))
+            return DQ_ERR_UNSUPPORTED;
     }
     return DQ_OK;
 }
@@ -371,9 +375,9 @@ cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t coun
 }
 
 // A list that one cluster does in one launch.  (A tensor in rows on either side takes two entries of the table.)
-bool is_short(uint32_t count, uint64_t total)
+bool is_short(uint32_t count, uint64_t total, uint64_t most)
 {
-    return total == 0u || (total <= kShortElements && 2u * (uint64_t)count <= (uint64_t)kMiddle<kScale>);
+    return total == 0u || (total <= most && 2u * (uint64_t)count <= (uint64_t)kMiddle<kScale>);
 }
 
 constexpr int kMaxDevices = 64;
@@ -524,7 +528,7 @@ dq_status norm_of(const dq_tensor* list, uint32_t count, const ListInfo& info, f
         e = launch_parts<MAX, true>(list, count, tile_len, sms, ~0ull, slots, &num_slots, first_slot, st);
         if (e == cudaSuccess)
             e = launch_join_each<MAX>(count, first_slot, slots, num_slots, out_norm, out_norms, status, st);
-    } else if (is_short(count, info.total)) {
+    } else if (is_short(count, info.total, kShortNorm)) {
         dq::ClipArgs a = {};
         a.out_norm = out_norm;
         a.status = status;
@@ -569,7 +573,7 @@ dq_status scale(const Job& job, void* workspace, cudaStream_t st)
         a.status = clip->status_word;
     }
     if (clip && !clip->norm) {
-        if (is_short(count, info.total)) {
+        if (is_short(count, info.total, kShortScale)) {
             const cudaError_t e = with_table<kScale>(src, dst, count, cluster_tile_length(info.total, count), &next, nullptr,
                                                      [&](const auto& t) { return launch_cluster<MAX, true>(t, a, st); });
             return e == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
@@ -622,7 +626,7 @@ dq_status check_clip(const dq_clip* clip)
 
 uint64_t workspace_bytes_for(uint32_t count, const ListInfo& info, bool each)
 {
-    if (!each && is_short(count, info.total)) return 0u;
+    if (info.total == 0u || (!each && is_short(count, info.total, std::min(kShortNorm, kShortScale)))) return 0u;
     // (tiles of a tensor in rows may be half as long, and every tensor may have two that are short)
     const uint64_t slots = each ? 2u * kEachTiles + kEachTiles / 8u + 2u * (uint64_t)count
                                 : (uint64_t)kMaxGrid * (2u * (uint64_t)count / (uint64_t)(kLarge<kNorm> - 1) + 1u);

@@ -24,13 +24,15 @@ SLACK = 1.0 + 2.0 ** -19
 FILL = 0.3125                       # what lies around the tensors; must stay
 
 # (sizes, ...): one launch by one cluster; the whole GPU; more tensors than a table of each size holds
-SHORT = [1]
 LISTS = {
     "one": [1],
     "few": [1, 2, 7, 8, 9, 31, 255, 256, 257],
     "tiles": [1023, 1024, 1025, 2047, 2048, 2049, 3 * 1024 + 5],
     "empties": [0, 5, 0, 0, 4097, 0],
     "short_most": [(1 << 19) - 8000] + [50] * 159,
+    "short_norm": [(1 << 19) - 50 * 127] + [50] * 127,          # the most that one launch takes
+    "short_scale": [50] * 100 + [(3 << 17) - 50 * 100],
+    "past_short": [3 << 17, 1],
     "tensors_161": [50 + 13 * i % 701 for i in range(161)],
     "tensors_700": [1 + 37 * i % 1500 for i in range(700)],
     "tensors_1900": [1 + 101 * i % 900 if i % 50 else 0 for i in range(1900)],
@@ -450,6 +452,8 @@ def test_other_layouts(dq):
         dq.grad_clip([column], 1.0, out=[])
     with pytest.raises(dq.DqError):
         dq.grad_clip([column, column], 1.0)
+    with pytest.raises(dq.DqError):
+        dq.grad_clip([column], 1.0, out=[column])
     with pytest.raises(dq.DqError):
         dq.grad_clip([column], -1.0)
     with pytest.raises(ValueError, match="elements"):

@@ -55,6 +55,8 @@ BAD_TENSORS = [
     (dict(row=1024, stride=0), INVALID),
     (dict(n=1 << 33, row=1 << 31, stride=(1 << 31) + 1), UNSUPPORTED),
     (dict(row=1024, stride=1 << 32), UNSUPPORTED),
+    (dict(n=1 << 33, row=2, stride=(1 << 32) - 1), UNSUPPORTED),     # further apart than addresses go
+    (dict(data=1 << 57), UNSUPPORTED),
 ]
 
 
@@ -187,13 +189,51 @@ def test_workspace_sizes(dq):
     assert L.dq_grad_workspace_bytes(short, 1, 0) == 0
     assert L.dq_grad_workspace_bytes(short, 1, 1) > 0
     assert L.dq_grad_workspace_bytes(long, 1, 0) > 0
+    for each in (0, 1):
+        assert L.dq_grad_workspace_bytes(_list(dq, _t(dq, n=0)), 1, each) == 0
     assert L.dq_grad_workspace_bytes(None, 0, 0) == 0
     many = (dq.DqTensor * 5000)(*[_t(dq, n=7)] * 5000)
     assert L.dq_grad_workspace_bytes(many, 5000, 0) > L.dq_grad_workspace_bytes(long, 1, 0)
 
 
 class _Stream:
-    cuda_stream = 0
+    cuda_stream = 0x1230
+
+
+class _FakeCalls:
+    """In the place of the native calls: every call succeeds without a GPU."""
+    grad_norm = grad_clip = grad_gather = grad_scatter = staticmethod(lambda *a: 0)
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_outputs_are_allocated_on_the_stream_of_the_call(dq, monkeypatch, given):
+    import contextlib
+    entered, allocated_in = [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        entered.append(stream)
+        yield
+        entered.pop()
+
+    def new_output(numel, dtype, device):
+        allocated_in.append((numel, list(entered)))
+        return torch.empty(numel, dtype=dtype)
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda ptr, device: ("stream", ptr))
+    monkeypatch.setattr(dq.binding, "new_output", new_output)
+    monkeypatch.setattr(dq.binding, "_calls_module", _FakeCalls)
+    g, s = [torch.zeros(3, 4), torch.zeros(5)], _Stream if given else None
+    where = [("stream", 0x1230)] if given else []
+    norm = torch.ones(1)
+    for call, sizes in ((lambda: dq.grad_norm(g, stream=s), [1]), (lambda: dq.grad_clip(g, 1.0, stream=s), [1]),
+                        (lambda: dq.grad_gather(g, stream=s), [17]), (lambda: dq.grad_norm(g, out_norm=norm, stream=s), []),
+                        (lambda: dq.grad_clip(g, 1.0, norm=norm, stream=s), [])):
+        allocated_in.clear()
+        call()
+        assert allocated_in == [(n, where) for n in sizes]
+    assert dq.grad_clip(g, 1.0, norm=norm, stream=s) is norm
 
 
 def test_the_binding_refuses_what_is_no_list_of_gradients(dq):
