@@ -26,7 +26,8 @@
  *     caller.  The library allocates no device memory at run time and keeps no state between calls, with two
  *     exceptions that live in its device image: one error word per GPU (dq_device_error_flags) and the
  *     fixed staging array of dqsg_encode_host_static.  (Long *_host calls, but not that one, also keep a stream and two
- *     events per host thread and device, given back when the thread ends.)  It is asynchronous on the given stream (it never
+ *     events per host thread and device, given back when the thread ends; calls on lists of some hundred tensors and more keep
+ *     host memory of 200 bytes per tensor in the same way.)  It is asynchronous on the given stream (it never
  *     synchronises), except for the *_host entry points, which return after the results are in the
  *     caller's host buffers.
  *   - Outputs must not alias inputs.  Inputs are assumed finite.

@@ -4,7 +4,7 @@
 // argument conversions), five times what the library call itself takes; a kernel for a small gradient is done in
 // less.  Here the same work takes 0.3 us for an encode, and 0.4 us plus 0.1 us per message for a decode.  The GIL is
 // released around the library call, which may block while the stream's launch queue is full.  A list of gradients costs
-// 30 ns per tensor.
+// 14 ns per tensor, and 9 more where it is written.
 //
 // Every function returns the dq_status; errors of the arguments' types raise TypeError, as the ctypes calls do.  What torch
 // throws while a tensor is looked at (one under vmap has no storage, for instance) is raised as the Python exception
