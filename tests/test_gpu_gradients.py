@@ -686,3 +686,67 @@ def test_clipping_a_message_clips_its_gradient(dq, nested):
     want_packed, want_scale = encode(clipped, 1, 0, 0, p)
     assert torch.equal(clipped, g * 0.25)
     assert torch.equal(packed, want_packed) and torch.equal(scale, want_scale)
+
+
+# ------------------------------------------------------------------------------------------------------ random lists
+def _random_tensor(rng, g):
+    """(tensor, buffer around it): contiguous at any address, or a block of a matrix."""
+    dtype = rng.choice([F32, BF16, F16])
+    if rng.random() < 0.6:
+        n = rng.choice([0, 1, rng.randint(1, 40), rng.randint(1, 3000), rng.randint(1, 60_000), rng.randint(1, 700_000)])
+        at = rng.randint(0, 17)
+        buf = torch.randn(at + n + 20, device="cuda", generator=g).to(dtype)
+        return buf[at:at + n], buf
+    rows, row = rng.randint(1, 60), rng.choice([rng.randint(1, 30), 8 * rng.randint(1, 200), rng.randint(1, 5000)])
+    left, right = rng.choice([(0, 0), (8, 16), (rng.randint(0, 9), rng.randint(0, 9))])
+    buf = torch.randn(rows, left + row + right, device="cuda", generator=g).to(dtype)
+    return buf[:, left:left + row], buf
+
+
+def _around(t, buf):
+    """What of buf is not t's, as one tensor (t is a view of buf)."""
+    mask = torch.ones_like(buf, dtype=torch.bool)
+    mask.as_strided(t.shape, t.stride(), t.storage_offset()).fill_(False)
+    return buf[mask]
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_random_lists(dq, seed):
+    import random
+    rng = random.Random(seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    pairs = [_random_tensor(rng, g) for _ in range(rng.choice([1, 2, 5, 20, 90]))]
+    grads = [t for t, _ in pairs]
+    src = [t.contiguous().clone() for t in grads]
+    kind = rng.choice(["l2", "max"])
+    each, total = _norms([_f64(t) for t in src], kind)
+    norms = dq.binding.new_output(len(grads), F32, "cuda")
+    got = dq.grad_norm(grads, _kind(dq, kind), out_norms=norms)
+    _assert_norm(got, total, kind)
+    _assert_norm(dq.grad_norm(grads, _kind(dq, kind)), total, kind)
+    for v, w in zip(norms.tolist(), each):
+        _assert_norm(v, w, kind)
+    limit = float(np.float32(rng.choice([0.2, 0.9, 1.5]) * total))
+    # gather, and scatter of what was gathered into tensors of the same layouts
+    norm = torch.empty(1, device="cuda")
+    flat = dq.grad_gather(grads, max_norm=limit, kind=_kind(dq, kind), out_norm=norm)
+    n = sum(t.numel() for t in grads)
+    _assert_norm(norm, total, kind)
+    _assert_clipped([flat[:n]], [torch.cat([s.float().reshape(-1) for s in src])], norm, limit, total)
+    targets = [(b.clone(), t) for t, b in pairs]
+    out = [c.as_strided(t.shape, t.stride(), t.storage_offset()) for c, t in targets]
+    before = [_around(o, c).clone() for o, (c, _) in zip(out, targets)]
+    dq.grad_scatter(flat[:n], out)
+    for o, p in zip(out, flat[:n].split([t.numel() for t in grads])):
+        assert torch.equal(o.reshape(-1), p.to(o.dtype))
+    for o, (c, _), b in zip(out, targets, before):
+        assert torch.equal(_around(o, c), b)
+    # clipped into contiguous tensors of any type, and in place
+    to = [torch.empty(t.shape, dtype=rng.choice([F32, BF16, F16]), device="cuda") for t in grads]
+    norm = dq.grad_clip(grads, limit, out=to, kind=_kind(dq, kind))
+    _assert_clipped(to, src, norm, limit, total)
+    before = [_around(t, b).clone() for t, b in pairs]
+    norm = dq.grad_clip(grads, limit, kind=_kind(dq, kind))
+    _assert_clipped([t.contiguous() for t in grads], src, norm, limit, total)
+    for (t, b), w in zip(pairs, before):
+        assert torch.equal(_around(t, b), w)
