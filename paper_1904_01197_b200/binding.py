@@ -451,13 +451,14 @@ def grad_gather(grads: Sequence[torch.Tensor], out_flat: Optional[torch.Tensor] 
                 norm: Optional[torch.Tensor] = None, kind: int = DQ_NORM_L2, out_norm: Optional[torch.Tensor] = None,
                 status_word: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The tensors, one after the other, as the flat fp32 vector that an encoder takes; clipped on the way if `max_norm` is
-    given (`norm`, `kind`, `out_norm` and `status_word` as in grad_clip)."""
+    given (`norm`, `kind`, `out_norm` and `status_word` as in grad_clip).  `out_flat` has as many elements as the tensors
+    together; where those have none, it may be of any size and stays as it is."""
     if out_flat is None:
         if not len(grads):
             raise ValueError("grad_gather: an empty list needs its output tensor")
         n = sum(g.numel() for g in grads)
         with _allocating_for(stream, grads[0].device):
-            out_flat = new_output(max(1, n), torch.float32, grads[0].device)
+            out_flat = new_output(n, torch.float32, grads[0].device)
     _check((_calls_module or _calls()).grad_gather(grads, out_flat, max_norm, norm, kind, out_norm, status_word, stream),
            "dq_grad_gather")
     return out_flat

@@ -750,3 +750,13 @@ def test_random_lists(dq, seed):
     _assert_clipped([t.contiguous() for t in grads], src, norm, limit, total)
     for (t, b), w in zip(pairs, before):
         assert torch.equal(_around(t, b), w)
+
+
+def test_empty_tensors_gather_into_an_empty_vector_and_back(dq):
+    e = [torch.empty(0, device="cuda"), torch.empty(0, 5, dtype=BF16, device="cuda")]
+    norm = torch.full((1,), 9.0, device="cuda")
+    for kw in ({}, dict(max_norm=1.0, out_norm=norm)):
+        flat = dq.grad_gather(e, **kw)
+        assert flat.numel() == 0 and flat.dtype == F32 and flat.is_cuda
+        dq.grad_scatter(flat, e, **kw)
+    assert float(norm) == 0.0

@@ -294,3 +294,10 @@ def test_the_binding_refuses_other_kinds_of_tensors(dq):
     lines = r.stdout.split("\n")
     assert lines[:3] == ["int refused", "double refused", "sparse refused"], r.stdout
     assert "vmap raised True" in lines, r.stdout
+
+
+def test_a_list_of_empty_tensors_gathers_into_an_empty_vector(dq, monkeypatch):
+    """Not one element, which nothing would have written."""
+    monkeypatch.setattr(dq.binding, "_calls_module", _FakeCalls)
+    for grads in ([torch.zeros(0)], [torch.zeros(0), torch.zeros(3, 0)]):
+        assert dq.grad_gather(grads, stream=None).numel() == 0
