@@ -103,8 +103,9 @@ typedef struct {
  * GPU has room (the tail of one runs beside the head of the next), while a later kernel that waits for this
  * one still sees both complete.  Results are identical with and without the flag.
  * "Neither reads nor writes" is about the memory, not the pointer: a buffer that a stream-ordered allocator
- * hands out may be memory that the previous kernel still reads (its input, freed by the host a moment ago);
- * such a buffer is not free in this sense.
+ * hands out may be memory that the previous kernel still reads (its input, freed by the host a moment ago) or
+ * writes (its output, dropped unread, such as the norm of a call on a list of tensors); such a buffer is not free in
+ * this sense.  The workspace of such a call is: it may be given back, and handed out again, once the call has returned.
  */
 #define DQ_FLAG_OUTPUT_FREE 0x2u
 /*

@@ -599,6 +599,7 @@ dq_status scale(const Job& job, void* workspace, cudaStream_t st)
             float* norm = a.out_norm ? a.out_norm : static_cast<float*>(workspace);
             if (launch_join<MAX>(slots, a.num_slots, norm, a.status, st) != cudaSuccess) return DQ_ERR_CUDA;
             a.norm = norm;
+            a.norm_in_workspace = a.out_norm ? 0u : 1u;
             a.num_slots = 0u;
             a.out_norm = nullptr;
             a.status = nullptr;

@@ -516,7 +516,8 @@ __device__ __forceinline__ void publish_norm(float norm, float* out_norm, uint32
 // A part of the norm per CTA (slots[blockIdx]), or with EACH per tile (slots[tile]).  One wave of four CTAs per SM (64
 // registers: 128 KB in flight per SM).  Bound by HBM: with the join behind it 124 M bf16 elements take 39.5 us (6.3 TB/s), 124 M
 // fp32 72 us (6.9 TB/s), 25.6 M fp32 20 us (5.1 TB/s: 5 us are launch, ramp and join).  Five CTAs spill, CTAs of 1024 threads are
-// 1 us slower on short lists, more waves no faster.
+// 1 us slower on short lists, more waves no faster.  (The next kernel is one of the same call, which waits: it may be let in at
+// once.)
 template <class Table, bool ROWS, bool MAX, bool EACH>
 __global__ void __launch_bounds__(kGradThreads, kGradNormCtas)
 grad_norm_kernel(const __grid_constant__ Table t, NormPart<MAX>* slots)
@@ -563,7 +564,10 @@ __device__ __forceinline__ void join_slots(NormPart<MAX>& acc, const NormPart<MA
 }
 
 // The whole from the slots of all launches before it (CTA 0, where `out_norm` is given), and the norms of single tensors
-// from the slots of their tiles, a warp each: tensor i of the launch owns the slots [first[i], first[i + 1]).
+// from the slots of their tiles, a warp each: tensor i of the launch owns the slots [first[i], first[i + 1]).  The slots lie in
+// the call's workspace, which the caller may have given back by now, and the next kernel may be an encode that has been handed
+// that memory and stores without waiting (EncodeArgs::early_store): this kernel lets it in by its end only.  (Norms of 25.6 M fp32
+// elements back to back 21.8 us; let in behind the last read of a slot 22.8, and at once, which is not sound, 20.7.)
 constexpr int kGradJoinThreads = 1024;
 
 template <int N>
@@ -580,7 +584,6 @@ grad_norm_join_kernel(const __grid_constant__ Table t, const NormPart<MAX>* slot
 {
     __shared__ NormPart<MAX> parts[kGradJoinThreads / 32];
     grid_dependency_wait();
-    grid_dependency_launch_next();
     NormPart<MAX> acc = {};
     if (blockIdx.x == 0u) {
         if (!out_norm) return;
@@ -607,6 +610,7 @@ struct ClipArgs {
     uint32_t* status;            // optional
     uint16_t in_place;           // the destination is the source
     uint16_t max_kind;           // the slots are maxima
+    uint16_t norm_in_workspace;  // `norm` is not the caller's
 };
 
 __device__ __forceinline__ float clip_factor(float norm, float max_norm)
@@ -879,6 +883,11 @@ grad_scale_kernel(const __grid_constant__ Table t, const __grid_constant__ ClipA
         const float norm = *a.norm;
         c = clip_factor(norm, a.max_norm);
         if (blockIdx.x == 0u && threadIdx.x == 0u) publish_norm(norm, a.out_norm, a.status);
+        if (a.norm_in_workspace) {
+            // one thread lets the next kernel in for its CTA: not before all have their factor (see grad_norm_join_kernel)
+            asm volatile("" ::"f"(c));
+            __syncthreads();
+        }
     }
     grid_dependency_launch_next();
     if (a.in_place && c == 1.0f) return;

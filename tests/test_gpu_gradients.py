@@ -760,3 +760,54 @@ def test_empty_tensors_gather_into_an_empty_vector_and_back(dq):
         assert flat.numel() == 0 and flat.dtype == F32 and flat.is_cuda
         dq.grad_scatter(flat, e, **kw)
     assert float(norm) == 0.0
+
+
+def _described(dq, tensors):
+    kinds = {F32: dq.DQ_F32, BF16: dq.DQ_BF16, F16: dq.DQ_F16}
+    return (dq.DqTensor * len(tensors))(*[dq.DqTensor(t.data_ptr(), t.numel(), 0, 0, kinds[t.dtype], 0) for t in tensors])
+
+
+@pytest.mark.parametrize("call", ["norms", "gather_many"])
+def test_an_encode_that_stores_early_may_have_the_memory_of_the_workspace(dq, call):
+    """The workspace of a call goes back to the allocator when the call returns; an encode whose flags let it store before
+    its predecessor is complete may be handed that memory for its message."""
+    flags = dq.DQ_FLAG_INPUT_READY | dq.DQ_FLAG_OUTPUT_FREE
+    sizes = [1500] * 2000 if call == "gather_many" else [40_000] * 300
+    b = _gradients(sizes, _dtypes(sizes, F32), seed=12)
+    src = torch.cat(b.parts)
+    ws = int(dq.lib().dq_grad_workspace_bytes(_described(dq, b.parts), len(sizes), 1 if call == "norms" else 0))
+    assert ws > 0
+    n, plain, early = 16 * (ws // 4) - 5, dq.DqParams(512, 2, 3), dq.DqParams(512, 2, 3, 0, 0.0, 0.0, 0, flags)
+    g = torch.randn(n, device="cuda")
+    packed = torch.empty(dq.packed_words(n, 2), dtype=torch.int32, device="cuda")
+    scale = torch.empty(dq.num_buckets(n, 512), device="cuda")
+    dq.dqsg_encode(g, 5, 0, 1, plain, packed, scale)
+    want_packed, want_scale = packed.clone(), scale.clone()
+    norms, flat = torch.empty(len(sizes), device="cuda"), torch.empty(sum(sizes), device="cuda")
+    norm = torch.empty(1, device="cuda")
+    dq.grad_norm(b.parts, out_norm=norm, out_norms=norms)
+    want_norm, want_norms = norm.clone(), norms.clone()
+    want_flat = src * torch.tensor(_factor(norm, 1.0), device="cuda")
+    shared = 0
+    for _ in range(20):
+        norms.zero_()
+        flat.zero_()
+        scale.zero_()
+        probe = torch.empty(ws, dtype=torch.uint8, device="cuda")
+        at = probe.data_ptr()
+        del probe
+        if call == "norms":
+            dq.grad_norm(b.parts, out_norm=norm, out_norms=norms)
+        else:
+            dq.grad_gather(b.parts, flat, max_norm=1.0)
+        message = torch.empty(ws // 4, dtype=torch.int32, device="cuda")             # (nothing is enqueued by this)
+        shared += message.data_ptr() == at
+        dq.dqsg_encode(g, 5, 0, 1, early, message, scale)
+        torch.cuda.synchronize()
+        assert torch.equal(message[:want_packed.numel()], want_packed) and torch.equal(scale, want_scale)
+        if call == "norms":
+            assert torch.equal(norm, want_norm) and torch.equal(norms, want_norms)
+        else:
+            assert torch.equal(flat, want_flat)
+        del message
+    assert shared == 20

@@ -301,3 +301,23 @@ def test_a_list_of_empty_tensors_gathers_into_an_empty_vector(dq, monkeypatch):
     monkeypatch.setattr(dq.binding, "_calls_module", _FakeCalls)
     for grads in ([torch.zeros(0)], [torch.zeros(0), torch.zeros(3, 0)]):
         assert dq.grad_gather(grads, stream=None).numel() == 0
+
+
+def test_the_next_kernel_comes_in_after_the_last_read_of_a_workspace():
+    """The last kernel of a call reads the norm's parts, or the norm, from a workspace that is given back when the call
+    returns; an encode that stores without waiting may be handed that memory.  So a CTA may let the next kernel in only
+    behind a barrier that follows its last read, or by its end.  (grad_norm_kernel, which writes the parts, is followed by a
+    kernel of the same call, which waits for it; grad_cluster_kernel has no workspace.)"""
+    import re
+    source = (Path(__file__).resolve().parent.parent / "paper_1904_01197_b200" / "csrc" / "dq_grad.cuh").read_text()
+    source = re.sub(r"//[^\n]*", "", source)
+    kernels = {re.search(r"(\w+)\s*\(const __grid_constant__", k).group(1): k[:k.index("\n}\n")]
+               for k in source.split("__global__")[1:]}
+    assert set(kernels) == {"grad_norm_kernel", "grad_norm_join_kernel", "grad_scale_kernel", "grad_cluster_kernel"}
+    assert "launch_next" not in kernels["grad_norm_join_kernel"]
+    assert "a.norm" not in kernels["grad_cluster_kernel"] and "slots" not in kernels["grad_cluster_kernel"]
+    scale = kernels["grad_scale_kernel"]
+    lets_in = scale.index("grid_dependency_launch_next()")
+    assert lets_in > scale.index("grid_dependency_wait()") and scale.count("launch_next") == 1
+    reads = [m.start() for m in re.finditer(r"joined_norm<|\*a\.norm", scale)]
+    assert len(reads) == 3 and all("__syncthreads()" in scale[r:lets_in] for r in reads)
