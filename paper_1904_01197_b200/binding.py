@@ -414,7 +414,8 @@ def ternary_unpack(data: torch.Tensor, n: int, out: Optional[torch.Tensor] = Non
 # current one (without `stream` a call runs on that device's current stream).  They may be column blocks: rows of
 # contiguous elements at one distance; where the order of the elements does not matter (grad_norm, grad_clip in place or
 # into tensors of the same strides) any dense tensor will do.  Norms are fp32 tensors of one element on the device;
-# nothing is synchronised.
+# nothing is synchronised.  Nothing is differentiated either: tensors that require a gradient may be read at any time, and
+# written under torch.no_grad() only.
 def _one_on(stream, tensors, what):
     if not len(tensors):
         raise ValueError(f"{what}: an empty list needs its output tensor")

@@ -11,6 +11,7 @@
 // that the tensor's own methods raise.
 #include <Python.h>
 
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -270,6 +271,15 @@ PyObject* ternary_unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args)
 }
 
 // ------------------------------------------------------------------------------------------ gradients of many tensors
+// A tensor that a call is about to write.  No graph could tell of it: where torch would record one, a tensor that requires a
+// gradient is refused, as torch's own out= and in-place operations refuse it.  False: an exception is set.
+bool may_be_written(const at::Tensor& t, const char* what)
+{
+    if (!t.requires_grad() || !at::GradMode::is_enabled()) return true;
+    PyErr_Format(PyExc_RuntimeError, "%s: a tensor that requires a gradient is written under torch.no_grad() only", what);
+    return false;
+}
+
 // Which elements a tensor's description has to keep in order.
 enum class Order { kNone, kRows };
 
@@ -295,9 +305,12 @@ bool as_rows(const at::Tensor& t, dq_tensor* d)
     return true;
 }
 
+// Whether a call reads a tensor or writes it.
+enum class Use { kRead, kWrite };
+
 // A gradient tensor.  Where the order of its elements does not matter, any dense tensor is contiguous.  All tensors of a
 // call lie on one device.  False: an exception is set.
-bool as_gradient(PyObject* o, const char* what, Order order, c10::DeviceIndex* device, dq_tensor* d)
+bool as_gradient(PyObject* o, const char* what, Order order, Use use, c10::DeviceIndex* device, dq_tensor* d)
 {
     if (!THPVariable_Check(o)) {
         PyErr_Format(PyExc_TypeError, "%s: expected CUDA tensors", what);
@@ -316,6 +329,7 @@ bool as_gradient(PyObject* o, const char* what, Order order, c10::DeviceIndex* d
         return false;
     }
     *device = t.get_device();
+    if (use == Use::kWrite && !may_be_written(t, what)) return false;
     d->data = t.data_ptr();
     d->n = (uint64_t)t.numel();
     d->dtype = type == at::kFloat ? DQ_F32 : type == at::kBFloat16 ? DQ_BF16 : DQ_F16;
@@ -333,7 +347,7 @@ struct GradientList {
     std::vector<dq_tensor> t;
     ~GradientList() { Py_XDECREF(seq); }
 
-    bool take(PyObject* o, const char* what, Order order, c10::DeviceIndex* device)
+    bool take(PyObject* o, const char* what, Order order, Use use, c10::DeviceIndex* device)
     {
         if (THPVariable_Check(o)) {
             PyErr_Format(PyExc_TypeError, "%s: expected a list of tensors", what);
@@ -351,7 +365,7 @@ struct GradientList {
                 const char* next = reinterpret_cast<const char*>(THPVariable_Unpack(PyTuple_GET_ITEM(seq, i + 6)).unsafeGetTensorImpl());
                 for (int line = 0; line < 192; line += 64) __builtin_prefetch(next + line);
             }
-            if (!as_gradient(PyTuple_GET_ITEM(seq, i), what, order, device, &t[(size_t)i])) return false;
+            if (!as_gradient(PyTuple_GET_ITEM(seq, i), what, order, use, device, &t[(size_t)i])) return false;
         }
         return true;
     }
@@ -371,7 +385,8 @@ struct GradientList {
 };
 
 // A contiguous tensor of at least `least` elements on the call's device; None is a null pointer.
-bool buffer_pointer(PyObject* o, at::ScalarType type, const char* what, uint64_t least, c10::DeviceIndex* device, void** out)
+bool buffer_pointer(PyObject* o, at::ScalarType type, const char* what, Use use, uint64_t least, c10::DeviceIndex* device,
+                    void** out)
 {
     int64_t have = 0;
     *out = nullptr;
@@ -387,7 +402,7 @@ bool buffer_pointer(PyObject* o, at::ScalarType type, const char* what, uint64_t
         PyErr_Format(PyExc_ValueError, "%s: too small", what);
         return false;
     }
-    return true;
+    return use == Use::kRead || may_be_written(THPVariable_Unpack(o), what);
 }
 
 // The call's device is current while one of these lives, the stream is resolved on it (None: its current stream), and the
@@ -419,9 +434,9 @@ bool as_clip(PyObject* max_norm, PyObject* norm, PyObject* kind, PyObject* out_n
 {
     void *given, *out, *st;
     uint32_t k;
-    if (!as_u32(kind, &k) || !buffer_pointer(norm, at::kFloat, "norm", 1, device, &given) ||
-        !buffer_pointer(out_norm, at::kFloat, "out_norm", 1, device, &out) ||
-        !buffer_pointer(status, at::kInt, "status_word", 1, device, &st))
+    if (!as_u32(kind, &k) || !buffer_pointer(norm, at::kFloat, "norm", Use::kRead, 1, device, &given) ||
+        !buffer_pointer(out_norm, at::kFloat, "out_norm", Use::kWrite, 1, device, &out) ||
+        !buffer_pointer(status, at::kInt, "status_word", Use::kWrite, 1, device, &st))
         return false;
     *clips = max_norm != Py_None;
     clip->max_norm = 0.0f;
@@ -441,13 +456,13 @@ bool as_clip(PyObject* max_norm, PyObject* norm, PyObject* kind, PyObject* out_n
 }
 
 // The flat vector of a gather or scatter.
-bool as_flat(PyObject* o, const char* what, uint64_t total, c10::DeviceIndex* device, void** out)
+bool as_flat(PyObject* o, const char* what, Use use, uint64_t total, c10::DeviceIndex* device, void** out)
 {
     if (o == Py_None) {
         PyErr_Format(PyExc_TypeError, "%s: expected a contiguous CUDA tensor of torch.float32", what);
         return false;
     }
-    if (!buffer_pointer(o, at::kFloat, what, total, device, out)) return false;
+    if (!buffer_pointer(o, at::kFloat, what, use, total, device, out)) return false;
     if (total != 0 && (uint64_t)THPVariable_Unpack(o).numel() != total) {
         PyErr_Format(PyExc_ValueError, "%s: has %lld elements, the list has %llu", what,
                      (long long)THPVariable_Unpack(o).numel(), (unsigned long long)total);
@@ -465,10 +480,10 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     uint32_t kind;
     void *norm, *norms, *status;
     OnDevice on;
-    if (!g.take(a[0], "grads", Order::kNone, &device) || !as_u32(a[1], &kind) ||
-        !buffer_pointer(a[2], at::kFloat, "out_norm", 1, &device, &norm) ||
-        !buffer_pointer(a[3], at::kFloat, "out_norms", g.t.size(), &device, &norms) ||
-        !buffer_pointer(a[4], at::kInt, "status_word", 1, &device, &status) || !on.enter(device, a[5]))
+    if (!g.take(a[0], "grads", Order::kNone, Use::kRead, &device) || !as_u32(a[1], &kind) ||
+        !buffer_pointer(a[2], at::kFloat, "out_norm", Use::kWrite, 1, &device, &norm) ||
+        !buffer_pointer(a[3], at::kFloat, "out_norms", Use::kWrite, g.t.size(), &device, &norms) ||
+        !buffer_pointer(a[4], at::kInt, "status_word", Use::kWrite, 1, &device, &status) || !on.enter(device, a[5]))
         return nullptr;
     on.allocate(dq_grad_workspace_bytes(g.t.data(), g.count(), norms != nullptr));
     dq_status s;
@@ -495,9 +510,9 @@ PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         PyErr_SetString(PyExc_TypeError, "max_norm: expected a number");
         return nullptr;
     }
-    if (!g.take(a[0], "grads", Order::kNone, &device)) return nullptr;
+    if (!g.take(a[0], "grads", Order::kNone, in_place ? Use::kWrite : Use::kRead, &device)) return nullptr;
     if (!in_place) {
-        if (!o.take(a[2], "out", Order::kNone, &device)) return nullptr;
+        if (!o.take(a[2], "out", Order::kNone, Use::kWrite, &device)) return nullptr;
         if (o.t.size() != g.t.size()) {
             PyErr_SetString(PyExc_ValueError, "out: one tensor for each of grads");
             return nullptr;
@@ -542,7 +557,8 @@ PyObject* grad_gather(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     bool clips;
     void* flat;
     OnDevice on;
-    if (!g.take(a[0], "grads", Order::kRows, &device) || !as_flat(a[1], "out_flat", g.total(), &device, &flat) ||
+    if (!g.take(a[0], "grads", Order::kRows, Use::kRead, &device) ||
+        !as_flat(a[1], "out_flat", Use::kWrite, g.total(), &device, &flat) ||
         !as_clip(a[2], a[3], a[4], a[5], a[6], &device, &clip, &clips) || !on.enter(device, a[7]))
         return nullptr;
     THPVariable_Unpack(a[1]).unsafeGetTensorImpl()->bump_version();
@@ -566,7 +582,8 @@ PyObject* grad_scatter(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     bool clips;
     void* flat;
     OnDevice on;
-    if (!o.take(a[1], "out", Order::kRows, &device) || !as_flat(a[0], "flat", o.total(), &device, &flat) ||
+    if (!o.take(a[1], "out", Order::kRows, Use::kWrite, &device) ||
+        !as_flat(a[0], "flat", Use::kRead, o.total(), &device, &flat) ||
         !as_clip(a[2], a[3], a[4], a[5], a[6], &device, &clip, &clips) || !on.enter(device, a[7]))
         return nullptr;
     o.written();

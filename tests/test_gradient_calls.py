@@ -1,6 +1,7 @@
 """Calls on gradients of many tensors, without a GPU: what the C ABI refuses before it launches anything, what the binding
 refuses, and the sizes of the workspace."""
 import ctypes as C
+import os
 import subprocess
 import sys
 from pathlib import Path
@@ -321,3 +322,50 @@ def test_the_next_kernel_comes_in_after_the_last_read_of_a_workspace():
     assert lets_in > scale.index("grid_dependency_wait()") and scale.count("launch_next") == 1
     reads = [m.start() for m in re.finditer(r"joined_norm<|\*a\.norm", scale)]
     assert len(reads) == 3 and all("__syncthreads()" in scale[r:lets_in] for r in reads)
+
+
+_FAKE_GRAD_MODE = _FAKES.split("    f32, one, other =")[0] + """
+    x, out, one, flat = new(8), new(8), new(1), new(8)
+    leaf, word, vector = new(8).requires_grad_(), new(1).requires_grad_(), new(8).requires_grad_()
+    result = leaf * 2
+    S = dict(stream=Stream)
+    def outcome(name, call):
+        try:
+            call()
+        except RuntimeError as e:                       # (without a GPU: what else there is to complain of is the missing driver)
+            print(name, "refused" if "requires a gradient" in str(e) else "not refused")
+    for name, call in (
+            ("leaf in place", lambda: dq.grad_clip([x, leaf], 1.0, out_norm=one, **S)),
+            ("result in place", lambda: dq.grad_clip([result], 1.0, out_norm=one, **S)),
+            ("leaf as out", lambda: dq.grad_clip([x, x], 1.0, out=[out, leaf], out_norm=one, **S)),
+            ("view of a leaf", lambda: dq.grad_clip([x[:4]], 1.0, out=[leaf[:4]], out_norm=one, **S)),
+            ("scatter", lambda: dq.grad_scatter(flat, [leaf], **S)),
+            ("flat", lambda: dq.grad_gather([x], vector, **S)),
+            ("norm", lambda: dq.grad_norm([x], out_norm=word, **S)),
+            ("norm of a clip", lambda: dq.grad_clip([x], 1.0, out_norm=word, **S)),
+            ("norms", lambda: dq.grad_norm([x] * 8, out_norm=one, out_norms=vector, **S))):
+        outcome(name, call)
+        with torch.no_grad():                           # where nothing is recorded it is an ordinary tensor
+            outcome("no_grad " + name, call)
+    # what is only read may require a gradient
+    for name, call in (("read norm", lambda: dq.grad_norm([leaf, result], out_norm=one, **S)),
+                       ("read gather", lambda: dq.grad_gather([leaf], flat, **S)),
+                       ("read clip", lambda: dq.grad_clip([leaf], 1.0, out=[out], norm=word, **S))):
+        outcome(name, call)
+"""
+
+
+def _without_gpu(script):
+    """The output of a script on fake tensors, whose addresses no GPU may see."""
+    r = subprocess.run([sys.executable, "-c", script, str(Path(__file__).resolve().parent.parent)], capture_output=True,
+                       text=True, timeout=300, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""})
+    assert r.returncode == 0, r.stderr[-2000:]
+    return [x for x in r.stdout.split("\n") if x]
+
+
+def test_tensors_that_require_a_gradient_are_written_in_no_grad_only(dq):
+    lines = _without_gpu(_FAKE_GRAD_MODE)
+    want = ["leaf in place", "result in place", "leaf as out", "view of a leaf", "scatter", "flat", "norm", "norm of a clip",
+            "norms"]
+    assert lines == [x for w in want for x in (w + " refused", "no_grad " + w + " not refused")] + [
+        "read norm not refused", "read gather not refused", "read clip not refused"], lines
