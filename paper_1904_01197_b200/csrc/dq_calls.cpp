@@ -13,6 +13,7 @@
 
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -272,13 +273,28 @@ PyObject* ternary_unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args)
 
 // ------------------------------------------------------------------------------------------ gradients of many tensors
 // A tensor that a call is about to write.  No graph could tell of it: where torch would record one, a tensor that requires a
-// gradient is refused, as torch's own out= and in-place operations refuse it.  False: an exception is set.
+// gradient is refused, as torch's own out= and in-place operations refuse it, and an inference tensor wherever it may not
+// be written.  False: an exception is set.
 bool may_be_written(const at::Tensor& t, const char* what)
 {
-    if (!t.requires_grad() || !at::GradMode::is_enabled()) return true;
-    PyErr_Format(PyExc_RuntimeError, "%s: a tensor that requires a gradient is written under torch.no_grad() only", what);
+    if (t.requires_grad() && at::GradMode::is_enabled())
+        PyErr_Format(PyExc_RuntimeError, "%s: a tensor that requires a gradient is written under torch.no_grad() only", what);
+    else if (t.is_inference() && !c10::InferenceMode::is_enabled())
+        PyErr_Format(PyExc_RuntimeError, "%s: an inference tensor is written under torch.inference_mode() only", what);
+    else
+        return true;
     return false;
 }
+
+// Autograd notices that a tensor it has saved was written.  (None: nothing was.)
+void mark_written(const at::Tensor& t) { t.unsafeGetTensorImpl()->bump_version(); }
+void mark_written(PyObject* o)
+{
+    if (o != Py_None) mark_written(THPVariable_Unpack(o));
+}
+
+// What the library refuses, it has not touched.
+bool was_refused(dq_status s) { return s != DQ_OK && s != DQ_ERR_CUDA; }
 
 // Which elements a tensor's description has to keep in order.
 enum class Order { kNone, kRows };
@@ -377,10 +393,9 @@ struct GradientList {
         for (const dq_tensor& x : t) n += x.n;
         return n;
     }
-    // (autograd notices that a tensor it has saved was written)
-    void written() const
+    void mark_all_written() const
     {
-        for (size_t i = 0; i < t.size(); ++i) tensor(i).unsafeGetTensorImpl()->bump_version();
+        for (size_t i = 0; i < t.size(); ++i) mark_written(tensor(i));
     }
 };
 
@@ -493,6 +508,9 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args)
                          static_cast<float*>(norms), static_cast<uint32_t*>(status), on.workspace,
                          on.memory ? (uint64_t)on.memory->numel() : 0, on.stream);
     }
+    if (!was_refused(s)) {
+        for (int i = 2; i < 5; ++i) mark_written(a[i]);
+    }
     return PyLong_FromLong(s);
 }
 
@@ -536,13 +554,17 @@ PyObject* grad_clip(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         }
     }
     if (!as_clip(a[1], a[3], a[4], a[5], a[6], &device, &clip, &clips) || !on.enter(device, a[7])) return nullptr;
-    (in_place ? g : o).written();
     if (!clip.norm) on.allocate(dq_grad_workspace_bytes(g.t.data(), g.count(), 0));
     dq_status s;
     {
         WithoutGil released;
         s = dq_grad_clip(g.t.data(), g.count(), &clip, in_place ? nullptr : o.t.data(), on.workspace,
                          on.memory ? (uint64_t)on.memory->numel() : 0, on.stream);
+    }
+    if (!was_refused(s)) {
+        (in_place ? g : o).mark_all_written();
+        mark_written(a[5]);
+        mark_written(a[6]);
     }
     return PyLong_FromLong(s);
 }
@@ -561,13 +583,15 @@ PyObject* grad_gather(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         !as_flat(a[1], "out_flat", Use::kWrite, g.total(), &device, &flat) ||
         !as_clip(a[2], a[3], a[4], a[5], a[6], &device, &clip, &clips) || !on.enter(device, a[7]))
         return nullptr;
-    THPVariable_Unpack(a[1]).unsafeGetTensorImpl()->bump_version();
     if (clips && !clip.norm) on.allocate(dq_grad_workspace_bytes(g.t.data(), g.count(), 0));
     dq_status s;
     {
         WithoutGil released;
         s = dq_grad_gather(g.t.data(), g.count(), clips ? &clip : nullptr, static_cast<float*>(flat), on.workspace,
                            on.memory ? (uint64_t)on.memory->numel() : 0, on.stream);
+    }
+    if (!was_refused(s)) {
+        for (int i : {1, 5, 6}) mark_written(a[i]);
     }
     return PyLong_FromLong(s);
 }
@@ -586,13 +610,17 @@ PyObject* grad_scatter(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         !as_flat(a[0], "flat", Use::kRead, o.total(), &device, &flat) ||
         !as_clip(a[2], a[3], a[4], a[5], a[6], &device, &clip, &clips) || !on.enter(device, a[7]))
         return nullptr;
-    o.written();
     if (clips && !clip.norm) on.allocate(dq_grad_workspace_bytes(o.t.data(), o.count(), 0));
     dq_status s;
     {
         WithoutGil released;
         s = dq_grad_scatter(static_cast<const float*>(flat), clips ? &clip : nullptr, o.t.data(), o.count(), on.workspace,
                             on.memory ? (uint64_t)on.memory->numel() : 0, on.stream);
+    }
+    if (!was_refused(s)) {
+        o.mark_all_written();
+        mark_written(a[5]);
+        mark_written(a[6]);
     }
     return PyLong_FromLong(s);
 }

@@ -811,3 +811,51 @@ def test_an_encode_that_stores_early_may_have_the_memory_of_the_workspace(dq, ca
             assert torch.equal(flat, want_flat)
         del message
     assert shared == 20
+
+
+def test_every_output_is_marked_as_written_and_none_of_a_refused_call(dq):
+    x, y, z = (torch.ones(100, device="cuda") for _ in range(3))
+    flat, norms = torch.ones(200, device="cuda"), torch.ones(2, device="cuda")
+    norm, status = torch.ones(1, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    everything = dict(x=x, y=y, z=z, flat=flat, norms=norms, norm=norm, status=status)
+    words = dict(out_norm=norm, status_word=status)
+
+    def written(call):
+        before = {k: t._version for k, t in everything.items()}
+        try:
+            call()
+        except dq.DqError:
+            assert all(t._version == before[k] for k, t in everything.items())
+            return "refused"
+        return sorted(k for k, t in everything.items() if t._version > before[k])
+
+    assert written(lambda: dq.grad_norm([x, y], out_norms=norms, **words)) == ["norm", "norms", "status"]
+    assert written(lambda: dq.grad_norm([x, y], out_norm=norm)) == ["norm"]
+    assert written(lambda: dq.grad_clip([x, y], 1.0, **words)) == ["norm", "status", "x", "y"]
+    assert written(lambda: dq.grad_clip([x], 1.0, out=[z], norm=norm, status_word=status)) == ["status", "z"]
+    assert written(lambda: dq.grad_gather([x, y], flat, max_norm=1.0, **words)) == ["flat", "norm", "status"]
+    assert written(lambda: dq.grad_scatter(flat, [x, y], max_norm=1.0, **words)) == ["norm", "status", "x", "y"]
+    assert written(lambda: dq.grad_gather([x, y], flat)) == ["flat"]
+    assert written(lambda: dq.grad_scatter(flat, [x, y])) == ["x", "y"]
+    # refused by the library
+    assert written(lambda: dq.grad_norm([x, y], 7, out_norms=norms, **words)) == "refused"
+    assert written(lambda: dq.grad_clip([x, x], 1.0, **words)) == "refused"
+    assert written(lambda: dq.grad_clip([x, y], -1.0, **words)) == "refused"
+    assert written(lambda: dq.grad_clip([x], 1.0, out=[x], **words)) == "refused"
+    assert written(lambda: dq.grad_gather([flat[:100], y], flat, **words, max_norm=1.0)) == "refused"
+    assert written(lambda: dq.grad_scatter(flat, [flat[:100], y])) == "refused"
+
+
+def test_inference_tensors_are_written_in_inference_mode_only(dq):
+    with torch.inference_mode():
+        t = torch.full((4,), 3.0, device="cuda")
+        dq.grad_clip([t], 1.0)
+        assert t.tolist() == [0.5] * 4
+        norm = dq.grad_norm([t])
+    flat = dq.grad_gather([t])                          # (read at any time)
+    assert flat.tolist() == [0.5] * 4
+    for call in (lambda: dq.grad_clip([t], 0.1), lambda: dq.grad_scatter(flat, [t]), lambda: dq.grad_norm([flat], out_norm=norm),
+                 lambda: dq.grad_gather([flat], t)):
+        with pytest.raises(RuntimeError, match="inference"):
+            call()
+    assert t.tolist() == [0.5] * 4 and float(norm) == 1.0
