@@ -369,3 +369,123 @@ def test_tensors_that_require_a_gradient_are_written_in_no_grad_only(dq):
             "norms"]
     assert lines == [x for w in want for x in (w + " refused", "no_grad " + w + " not refused")] + [
         "read norm not refused", "read gather not refused", "read clip not refused"], lines
+
+
+# ------------------------------------------------------------------------------------------ overlap in large groups
+def _overlap_by_pairs(extents):
+    """The rule, pair by pair: extents are (start, end, width and pitch of a row in bytes (pitch 0: one piece), written)."""
+    order = sorted(extents, key=lambda x: x[0])
+    for k, (lo, _, width, pitch, out) in enumerate(order):
+        for a_lo, a_hi, a_width, a_pitch, a_out in order[:k]:
+            if not (out or a_out) or a_hi <= lo:
+                continue
+            if a_pitch == 0 or (pitch != 0 and pitch != a_pitch):
+                return True
+            column = (lo - a_lo) % a_pitch
+            if column < a_width or column + width > a_pitch:
+                return True
+    return False
+
+
+def _extent(t, out):
+    size = 4 if t.dtype == 0 else 2
+    if t.row and t.row_stride != t.row and t.row != t.n:
+        return t.data, t.data + size * ((t.n // t.row - 1) * t.row_stride + t.row), size * t.row, size * t.row_stride, out
+    return t.data, t.data + size * t.n, size * t.n, 0, out
+
+
+def _blocks_beside_each_other(dq, rng, base):
+    """Blocks of one matrix, with gaps, in bands of rows, and contiguous tensors in what a row leaves free."""
+    pitch, tensors, column = rng.choice([2000, 5000]), [], rng.randrange(0, 40)
+    while True:
+        width = rng.choice([1, 2, 7, 8, 30, 64])
+        if column + width > pitch:
+            break
+        row = 0
+        while row < 12:
+            rows = rng.randint(1, 6)
+            if rng.random() < 0.8:
+                tensors.append((base + 4 * (row * pitch + column), rows * width, width, pitch) if rows > 1
+                               else (base + 4 * (row * pitch + column), width, 0, 0))
+            row += rows
+        column += width + rng.choice([0, 0, 1, 5, 40])
+    rng.shuffle(tensors)
+    return [_t(dq, data=d, n=n, row=r, stride=s) for d, n, r, s in tensors]
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_overlap_in_a_large_group_is_found_as_pair_by_pair(dq, seed):
+    import random
+    rng = random.Random(seed)
+    seen = []
+    for _ in range(8):
+        blocks = _blocks_beside_each_other(dq, rng, BASE << 12)[:500]
+        lists = {"in place": (blocks, None)}
+        # inputs that overlap each other, in another matrix or in one of another pitch, into those
+        sources = [_t(dq, data=(BASE << 16) + 4 * rng.randrange(4000), n=b.n, row=b.row,
+                      stride=b.row_stride + rng.choice([0, 0, 3]) if b.row else 0, dtype=rng.choice([0, 1])) for b in blocks]
+        lists["overlapping inputs"] = (sources, blocks)
+        # inputs among the outputs: every other block is read, into tensors far away, and the rest into itself in place of those
+        half = len(blocks) // 2
+        far = [_t(dq, data=(BASE << 20) + 8192 * i, n=b.n) for i, b in enumerate(blocks[:half])]
+        near = [_t(dq, data=b.data, n=b.n, row=b.row, stride=b.row_stride) for b in blocks[:half]]
+        lists["inputs beside outputs"] = (near + [_t(dq, data=(BASE << 24) + 8192 * i, n=b.n)
+                                                  for i, b in enumerate(blocks[half:])], far + blocks[half:])
+        for name, (src, out) in lists.items():
+            assert len(src) > 128                       # (long lists: the workspace's fault stops a call that has no other)
+            for move in [0] + [rng.choice([-64, -8, -4, 4, 8, 28, 400, 8000, 20000, 20004]) for _ in range(6)]:
+                side = rng.choice([src, out or src])
+                k = rng.randrange(len(side))
+                side[k].data += move
+                extents = [_extent(t, out is None) for t in src] + [_extent(t, True) for t in out or []]
+                want = _overlap_by_pairs(extents)
+                got = _clip_status(dq, src, out)
+                assert got == (INVALID if want else NO_OVERLAP), (name, k, move)
+                seen.append(want)
+                side[k].data -= move
+    assert len(seen) > 100 and 0.2 < sum(seen) / len(seen) < 0.9
+
+
+@pytest.mark.parametrize("into", [False, True], ids=["in_place", "into_others"])
+@pytest.mark.parametrize("count", [1000, 4000, 65536])
+def test_many_blocks_of_one_matrix_are_checked_quickly(dq, count, into):
+    """Blocks of one matrix all reach over one another.  Pair by pair 65,536 of them took 9 s."""
+    import time
+    L = dq.lib()
+    blocks = [_t(dq, data=BASE + 32 * i, n=64, row=8, stride=8 * count) for i in range(count)]
+    others = [_t(dq, data=(BASE << 24) + 32 * i, n=64, row=8, stride=8 * count) for i in range(count)] if into else None
+    a, b = _list(dq, *blocks), _list(dq, *others) if into else None
+    written = b if into else a
+
+    def call():
+        start = time.perf_counter()
+        s = L.dq_grad_clip(a, count, _clip(dq), b, 0x208, 1 << 30, None)
+        return s, time.perf_counter() - start
+
+    assert call()[0] == NO_OVERLAP
+    took = min(call()[1] for _ in range(3))
+    assert took < 1e-3 + 4e-6 * count, took             # (measured: 0.3 to 0.5 us each)
+    # one block a column too wide or too far left, anywhere among them
+    for k, change in ((0, dict(row=9, n=72)), (count // 2, dict(row=9, n=72)), (count - 1, dict(data=-4)), (count // 3, dict(data=4))):
+        kept = written[k].data, written[k].n, written[k].row
+        written[k].data += change.get("data", 0)
+        written[k].row, written[k].n = change.get("row", 8), change.get("n", 64)
+        if into:
+            a[k].row, a[k].n, a[k].row_stride = 0, written[k].n, 0
+            a[k].data = BASE << 34
+        assert call()[0] == INVALID
+        written[k].data, written[k].n, written[k].row = kept
+        if into:
+            a[k].data, a[k].n, a[k].row, a[k].row_stride = BASE + 32 * k, 64, 8, 8 * count
+    assert call()[0] == NO_OVERLAP
+
+
+def test_many_inputs_that_overlap_each_other_are_checked_quickly(dq):
+    """They may; only outputs are compared with anything."""
+    import time
+    L = dq.lib()
+    count = 20_000
+    a = _list(dq, *[_t(dq, data=BASE + 4 * i, n=64, row=8, stride=4096 + (i % 3)) for i in range(count)])
+    start = time.perf_counter()
+    s = L.dq_grad_gather(a, count, _clip(dq), BASE << 24, 0x208, 1 << 30, None)
+    assert s == NO_OVERLAP and time.perf_counter() - start < 0.1
