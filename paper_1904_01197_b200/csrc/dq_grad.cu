@@ -529,8 +529,8 @@ bool entries_fit(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uin
     return entries <= most;
 }
 
-// Calls f(table) with the smallest table that holds the rest of the list.
-template <int W, class F>
+// Calls f(table) with the smallest table that holds the rest of the list; there is none larger than MOST entries.
+template <int W, int MOST = kLarge<W>, class F>
 cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t count, uint32_t tile_len, uint32_t* next,
                        uint32_t* first_slot, F&& f)
 {
@@ -540,12 +540,14 @@ cudaError_t with_table(const dq_tensor* src, const dq_tensor* dst, uint32_t coun
         fill(t, src, dst, count, tile_len, next, first_slot);
         return f(t);
     }
-    if (entries_fit(src + *next, to, count - *next, kMiddle<W>)) {
-        dq::GradTable<kMiddle<W>, W> t;
-        fill(t, src, dst, count, tile_len, next, first_slot);
-        return f(t);
+    if constexpr (MOST > kMiddle<W>) {
+        if (!entries_fit(src + *next, to, count - *next, kMiddle<W>)) {
+            dq::GradTable<MOST, W> t;
+            fill(t, src, dst, count, tile_len, next, first_slot);
+            return f(t);
+        }
     }
-    dq::GradTable<kLarge<W>, W> t;
+    dq::GradTable<kMiddle<W>, W> t;
     fill(t, src, dst, count, tile_len, next, first_slot);
     return f(t);
 }
@@ -595,6 +597,7 @@ uint32_t cluster_size()
 template <bool ROWS, bool MAX, bool SCALE, class Table>
 cudaError_t launch_cluster_of(const Table& t, const dq::ClipArgs& a, cudaStream_t st)
 {
+    static_assert(Table::kCapacity <= kMiddle<Table::kWords>, "short lists have no larger tables");
     const uint32_t most = cluster_size<Table, ROWS, MAX, SCALE>();
     if (most == 0u) return cudaErrorUnknown;
     // no CTA without a tile for every other warp
@@ -709,8 +712,8 @@ dq_status norm_of(const dq_tensor* list, uint32_t count, const ListInfo& info, f
         a.out_norm = out_norm;
         a.status = status;
         uint32_t next = 0u;
-        e = with_table<kNorm>(list, nullptr, count, cluster_tile_length(info.total, count), &next, nullptr,
-                              [&](const auto& t) { return launch_cluster<MAX, false>(t, a, st); });
+        e = with_table<kNorm, kMiddle<kNorm>>(list, nullptr, count, cluster_tile_length(info.total, count), &next, nullptr,
+                                              [&](const auto& t) { return launch_cluster<MAX, false>(t, a, st); });
     } else {
         e = launch_parts<MAX, false>(list, count, norm_tile_length(info, sms), sms, ~0ull, slots, &num_slots, nullptr, st);
         if (e == cudaSuccess) e = launch_join<MAX>(slots, num_slots, out_norm, status, st);
@@ -750,8 +753,9 @@ dq_status scale(const Job& job, void* workspace, cudaStream_t st)
     }
     if (clip && !clip->norm) {
         if (is_short(count, info.total, kShortScale)) {
-            const cudaError_t e = with_table<kScale>(src, dst, count, cluster_tile_length(info.total, count), &next, nullptr,
-                                                     [&](const auto& t) { return launch_cluster<MAX, true>(t, a, st); });
+            const cudaError_t e = with_table<kScale, kMiddle<kScale>>(
+                src, dst, count, cluster_tile_length(info.total, count), &next, nullptr,
+                [&](const auto& t) { return launch_cluster<MAX, true>(t, a, st); });
             return e == cudaSuccess ? DQ_OK : DQ_ERR_CUDA;
         }
         auto* slots = reinterpret_cast<dq::NormPart<MAX>*>(static_cast<char*>(workspace) + 16);
