@@ -371,6 +371,44 @@ def test_tensors_that_require_a_gradient_are_written_in_no_grad_only(dq):
         "read norm not refused", "read gather not refused", "read clip not refused"], lines
 
 
+_FAKE_DEVICES = _FAKES.split("    f32, one, other =")[0] + """
+    def on(d):
+        return dict(x=new(8, device=d), y=new(8, device=d), one=new(1, device=d), flat=new(16, device=d),
+                    status=new(1, dtype=torch.int32, device=d))
+    a, b = on("cuda:0"), on("cuda:1")
+    S = dict(stream=Stream)
+    def outcome(name, call):
+        try:
+            call()
+        except TypeError as e:
+            print(name, "refused" if "on one device" in str(e) else e)
+        except RuntimeError as e:                       # (the missing driver)
+            print(name, "not refused")
+    for p, q, where in ((a, b, "01"), (b, a, "10")):
+        outcome("norm list " + where, lambda: dq.grad_norm([p["x"], q["y"]], out_norm=p["one"], **S))
+        outcome("norm word " + where, lambda: dq.grad_norm([p["x"]], out_norm=q["one"], **S))
+        outcome("norms " + where, lambda: dq.grad_norm([p["x"]], out_norm=p["one"], out_norms=q["flat"], **S))
+        outcome("status " + where, lambda: dq.grad_norm([p["x"]], out_norm=p["one"], status_word=q["status"], **S))
+        outcome("clip list " + where, lambda: dq.grad_clip([p["x"], q["y"]], 1.0, out_norm=p["one"], **S))
+        outcome("clip out " + where, lambda: dq.grad_clip([p["x"]], 1.0, out=[q["y"]], out_norm=p["one"], **S))
+        outcome("clip norm " + where, lambda: dq.grad_clip([p["x"]], 1.0, norm=q["one"], **S))
+        outcome("clip out_norm " + where, lambda: dq.grad_clip([p["x"]], 1.0, out_norm=q["one"], **S))
+        outcome("gather list " + where, lambda: dq.grad_gather([p["x"], q["y"]], p["flat"], **S))
+        outcome("gather flat " + where, lambda: dq.grad_gather([p["x"], p["y"]], q["flat"], **S))
+        outcome("scatter list " + where, lambda: dq.grad_scatter(p["flat"], [p["x"], q["y"]], **S))
+        outcome("scatter flat " + where, lambda: dq.grad_scatter(q["flat"], [p["x"], p["y"]], **S))
+        outcome("one device", lambda: dq.grad_norm([p["x"], p["y"]], out_norm=p["one"], out_norms=p["flat"],
+                                                   status_word=p["status"], **S))
+"""
+
+
+def test_the_tensors_of_a_call_lie_on_one_device(dq):
+    lines = _without_gpu(_FAKE_DEVICES)
+    assert len(lines) == 26
+    assert all(x == "one device not refused" if x.startswith("one device") else x.endswith(" refused") for x in lines), lines
+    assert sum(x.endswith("not refused") for x in lines) == 2, lines
+
+
 # ------------------------------------------------------------------------------------------ overlap in large groups
 def _overlap_by_pairs(extents):
     """The rule, pair by pair: extents are (start, end, width and pitch of a row in bytes (pitch 0: one piece), written)."""
