@@ -859,3 +859,67 @@ def test_inference_tensors_are_written_in_inference_mode_only(dq):
         with pytest.raises(RuntimeError, match="inference"):
             call()
     assert t.tolist() == [0.5] * 4 and float(norm) == 1.0
+
+
+# ------------------------------------------------------------------------------------------------------ the largest lists
+@pytest.mark.parametrize("count", [8000, 8001, 20_000, 65_536])
+def test_lists_of_thousands(dq, count):
+    """Up to the most tensors of a call: several launches of every kernel, contiguous tensors and blocks of one matrix."""
+    g = torch.Generator(device="cuda").manual_seed(count)
+    whole = torch.randn(count, 7, device="cuda", generator=g)
+    each = dq.binding.new_output(count, F32, "cuda")
+
+    def check_norms(tensors, values):
+        total = dq.grad_norm(tensors, out_norms=each)
+        want = values.double().square().sum(1)
+        assert bool(((each.double() - want.sqrt()).abs() <= want.sqrt() * 2.0 ** -24 * SLACK).all())
+        _assert_norm(total, math.sqrt(math.fsum(want.tolist())), "l2")
+        assert torch.equal(dq.grad_norm(tensors, dq.DQ_NORM_MAX, out_norms=each), values.abs().max().reshape(1))
+        assert torch.equal(each, values.abs().amax(1))
+        return total
+
+    tensors = list(whole.unbind(0))
+    total = check_norms(tensors, whole)
+    c = torch.tensor(_factor(total, 0.5), device="cuda")
+    norm = torch.empty(1, device="cuda")
+    flat = dq.grad_gather(tensors, max_norm=0.5, out_norm=norm)
+    assert torch.equal(flat, whole.reshape(-1) * torch.tensor(_factor(norm, 0.5), device="cuda"))
+    assert torch.equal(dq.grad_gather(tensors, max_norm=0.5, norm=total), whole.reshape(-1) * c)
+    half = torch.empty(count, 7, dtype=BF16, device="cuda")
+    dq.grad_scatter(flat, list(half.unbind(0)), max_norm=0.25, out_norm=norm)
+    assert torch.equal(half.reshape(-1), (flat * torch.tensor(_factor(norm, 0.25), device="cuda")).to(BF16))
+    before = whole.clone()
+    norm = dq.grad_clip(tensors, 0.125)
+    assert torch.equal(whole, before * torch.tensor(_factor(norm, 0.125), device="cuda"))
+
+    matrix = torch.randn(5, count * 9, device="cuda", generator=g)
+    blocks = [matrix[:, 9 * i:9 * i + 8] for i in range(count)]
+    inside = matrix.clone().view(5, count, 9)[:, :, :8].transpose(0, 1)
+    check_norms(blocks, inside.reshape(count, 40))
+    assert torch.equal(dq.grad_gather(blocks), inside.reshape(-1))
+    want = matrix.clone()
+    norm = dq.grad_clip(blocks, 1.0)
+    want.view(5, count, 9)[:, :, :8] *= torch.tensor(_factor(norm, 1.0), device="cuda")
+    assert torch.equal(matrix, want)
+
+
+def test_gather_and_scatter_beyond_32_bits(dq):
+    n = (1 << 32) + 13
+    buf = torch.zeros(n + 64, dtype=BF16, device="cuda")
+    x, y = buf[3:3 + n], torch.tensor([9.0, 10.0], device="cuda")
+    spots = [0, 5, 1 << 31, (1 << 31) + 1, (1 << 32) - 1, 1 << 32, n - 9, n - 1]
+    for i, s in enumerate(spots):
+        x[s] = float(i + 1)
+    flat = torch.full((n + 2,), FILL, device="cuda")
+    norm = torch.empty(1, device="cuda")
+    dq.grad_gather([x, y], flat, max_norm=5.0, kind=dq.DQ_NORM_MAX, out_norm=norm)
+    assert float(norm) == 10.0
+    want = [0.5 * (i + 1) for i in range(8)]
+    assert [float(flat[s]) for s in spots] == want and flat[n:].tolist() == [4.5, 5.0]
+    assert int(torch.count_nonzero(flat)) == 10
+    buf.fill_(FILL)
+    back = torch.zeros(2, device="cuda")
+    dq.grad_scatter(flat, [x, back])
+    assert [float(x[s]) for s in spots] == want and back.tolist() == [4.5, 5.0]
+    assert int(torch.count_nonzero(x)) == 8
+    assert bool((buf[:3] == FILL).all()) and bool((buf[3 + n:] == FILL).all())
