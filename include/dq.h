@@ -27,9 +27,9 @@
  *     exceptions that live in its device image: one error word per GPU (dq_device_error_flags) and the
  *     fixed staging array of dqsg_encode_host_static.  (Long *_host calls, but not that one, also keep a stream and two
  *     events per host thread and device, given back when the thread ends; calls on lists of some hundred tensors and more keep
- *     host memory of 200 bytes per tensor in the same way.)  It is asynchronous on the given stream (it never
- *     synchronises), except for the *_host entry points, which return after the results are in the
- *     caller's host buffers.
+ *     host memory in the same way, less than 500 bytes per tensor of their longest list.)  It is asynchronous on the
+ *     given stream (it never synchronises), except for the *_host entry points, which return after the results are in
+ *     the caller's host buffers.
  *   - Outputs must not alias inputs.  Inputs are assumed finite.
  *   - The integer decisions are taken in fp32 with the rounding constant 1.5 * 2^23, which is exact for
  *     magnitudes below 2^22: DQSG needs (L-1)/2 + 1 < 2^22 (always true for b <= 8); NDQSG needs
@@ -307,12 +307,14 @@ typedef enum {
 
 /*
  * How a list is clipped: every element is multiplied in fp32 by c = 1 if N <= max_norm, else max_norm / N, and rounded once
- * to the destination's type.  N is the norm that the call computes of its input, or the one at `norm` (for instance of
- * all ranks' parts together).  A norm of Inf gives c = 0, a NaN gives c = NaN; finite gradients whose L2 norm is beyond
- * the fp32 range have the norm Inf.
+ * to the destination's type.  (Nothing is added to N, as some programs add 1e-6.)  N is the norm that the call computes of
+ * its input, or the one at `norm`: of all ranks' parts together, for instance, or of one replica where all have to clip by the
+ * same bits.  (The L2 norm of the same values may differ in its last fp32 bit where tensors lie at other addresses modulo 16
+ * bytes, or in another call: norm, norms of each tensor, clip.)  A norm of Inf gives c = 0 where max_norm is finite, a NaN
+ * always gives c = NaN; finite gradients whose L2 norm is beyond the fp32 range have the norm Inf.
  */
 typedef struct {
-    float        max_norm;     /* >= 0; Inf: nothing is clipped                                                */
+    float        max_norm;     /* >= 0; Inf: nothing is clipped, but by a norm that is NaN                      */
     dq_norm      kind;         /* of the norm that the call computes                                          */
     const float* norm;         /* device, fp32[1]: the norm to clip by; NULL: the call computes it             */
     float*       out_norm;     /* device, fp32[1], optional: receives N, the norm before clipping            */

@@ -15,7 +15,9 @@
 //
 // L2 sums run in fp64: an fp32 sum of 10^8 squares loses digits, and squares of fp32 values leave the fp32 range at
 // both ends.  Maxima are maxima of the bit patterns without the sign, where a NaN is above every number.  No atomics
-// are involved: the order of a sum depends on the sizes and the device only, not on timing.
+// are involved: the order of a sum does not depend on timing.  It does depend on how a call cuts its tensors up, that is on the
+// sizes, types, strides and addresses modulo 16 bytes (of the destination too, where one launch does all), on which call it is
+// and on the device: the same values elsewhere may have a norm that is one fp32 step away.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -514,10 +516,10 @@ __device__ __forceinline__ void publish_norm(float norm, float* out_norm, uint32
 }
 
 // A part of the norm per CTA (slots[blockIdx]), or with EACH per tile (slots[tile]).  One wave of four CTAs per SM (64
-// registers: 128 KB in flight per SM).  Bound by HBM: with the join behind it 124 M bf16 elements take 39.5 us (6.3 TB/s), 124 M
-// fp32 72 us (6.9 TB/s), 25.6 M fp32 20 us (5.1 TB/s: 5 us are launch, ramp and join).  Five CTAs spill, CTAs of 1024 threads are
-// 1 us slower on short lists, more waves no faster.  (The next kernel is one of the same call, which waits: it may be let in at
-// once.)
+// registers: 128 KB in flight per SM).  Bound by HBM: with the join behind it 124 M bf16 elements take 43.7 us (5.7 TB/s; their
+// maximum 40.6), 124 M fp32 78 us (6.4 TB/s), 25.6 M fp32 20.7 us (4.9 TB/s: 5 us are launch, ramp and join).  Five CTAs spill,
+// CTAs of 1024 threads are 1 us slower on short lists, more waves no faster.  (The next kernel is one of the same call, which
+// waits: it may be let in at once.)
 template <class Table, bool ROWS, bool MAX, bool EACH>
 __global__ void __launch_bounds__(kGradThreads, kGradNormCtas)
 grad_norm_kernel(const __grid_constant__ Table t, NormPart<MAX>* slots)
@@ -567,7 +569,8 @@ __device__ __forceinline__ void join_slots(NormPart<MAX>& acc, const NormPart<MA
 // from the slots of their tiles, a warp each: tensor i of the launch owns the slots [first[i], first[i + 1]).  The slots lie in
 // the call's workspace, which the caller may have given back by now, and the next kernel may be an encode that has been handed
 // that memory and stores without waiting (EncodeArgs::early_store): this kernel lets it in by its end only.  (Norms of 25.6 M fp32
-// elements back to back 21.8 us; let in behind the last read of a slot 22.8, and at once, which is not sound, 20.7.)
+// elements and of their 161 tensors, back to back: 21.8 us; let in behind the last read of a slot 22.8, and at once, which is
+// not sound, 20.7.)
 constexpr int kGradJoinThreads = 1024;
 
 template <int N>

@@ -25,10 +25,10 @@ using DecodeArgs = DecodeArgsOf<64>;
 // stream drains, which hides launch latency.  Every kernel executes griddepcontrol.wait before it writes anything, and
 // before it reads anything that the previous kernel may have produced -- unless the caller's flags say that an encode
 // need not (EncodeArgs::early_read, early_store), which they say about the previous kernel only.  Therefore at least one
-// CTA of every kernel executes griddepcontrol.launch_dependents only after its own wait: a kernel then starts when
-// everything before its predecessor is complete, and no more than two kernels ever overlap.  The last kernel of a call with a
-// workspace executes it only after its CTA's last access to that: the caller may have given the memory back by then, and an
-// encode that stores early may have been handed it.
+// CTA of every kernel executes griddepcontrol.launch_dependents (or ends) only after its own wait: a kernel then starts when
+// everything before its predecessor is complete, and no more than two kernels ever overlap.  In the
+// last kernel of a call with a workspace every CTA does so only after its last access to that: the caller may have given the
+// memory back by then, and an encode that stores early may have been handed it.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_overlapped(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, size_t smem, cudaStream_t st,
                               uint32_t cluster, Args&&... args)
